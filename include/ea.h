@@ -54,7 +54,9 @@ typedef enum ea_status {
     EA_ERR_WORKSPACE = 3,      /* context workspace smaller than ea_workspace_bytes    */
     EA_ERR_CUDA = 4,           /* a CUDA runtime call failed                           */
     EA_ERR_NOT_SM100 = 5,      /* device is not compute capability 10.x                */
-    EA_ERR_DEVICE_TIMEOUT = 6  /* a bounded device-side wait gave up                   */
+    EA_ERR_DEVICE_TIMEOUT = 6, /* a bounded device-side wait gave up                   */
+    EA_ERR_PAGES = 7           /* paged cache: lengths, offsets, slots or page numbers on
+                                  the device do not fit, or the pool is exhausted      */
 } ea_status;
 
 /* RoPE channel pairing used when the rotation is averaged (Eq. 6). */
@@ -513,6 +515,142 @@ ea_status ea_select_compact_adaptive(ea_ctx* ctx, const ea_shape* shape, const f
 int64_t ea_n_floor(int64_t n_kept, double safeguard);
 
 /*
+ * Paged cache: a home for compressed caches whose heads hold different numbers
+ * of pairs (the ragged output of ea_select_compact_adaptive), and the attention
+ * that reads it (the paper evaluates compression inside an ordinary attention
+ * layer and has no counterpart).
+ *
+ * A LIST is the cache of one (sequence, KV head): list r = s * Hkv + g.  K and V
+ * live in pools of pages of page_rows rows, bf16 [n_pages, page_rows, d] each;
+ * row p of list r sits in slot
+ *     block_table[r][p / page_rows] * page_rows + p % page_rows
+ * of both pools, row by row.  Lengths, tables, slots and the list of free pages
+ * are int32 in DEVICE memory, so a generation step can be captured into a CUDA
+ * graph; all checks of their values are made on the device: a call that finds
+ * some that do not fit records EA_ERR_PAGES, which ea_sync_status reports, and
+ * touches no memory outside the buffers described here.
+ *
+ * Limits (EA_ERR_UNSUPPORTED beyond): page_rows 16, 32, 64 or 128; head_dim 64,
+ * 128 or 256; n_seqs * n_kv_heads <= 65535; n_pages * page_rows and max_pages *
+ * page_rows < 2^31.  The calls that use the context's workspace need
+ * ea_paged_workspace_bytes (EA_ERR_WORKSPACE otherwise).  They end the validity
+ * of a fused statistics operand (ea_set_fused_stats), which lives there too.
+ */
+typedef struct ea_paged_shape {
+    int32_t n_seqs;      /* sequences in this call (or (layer, sequence) units)        */
+    int32_t n_q_heads;   /* Hq                                                         */
+    int32_t n_kv_heads;  /* Hkv, divides Hq                                            */
+    int32_t head_dim;    /* d: 64, 128 or 256                                          */
+    int32_t page_rows;   /* rows per page: 16, 32, 64 or 128                           */
+    int32_t n_pages;     /* pages in the pools                                         */
+    int32_t max_pages;   /* columns of the block table: pages a list may hold          */
+} ea_paged_shape;
+
+/* The order of a slot map's entries. */
+enum { EA_SLOTS_BY_LIST = 0,     /* list after list, rows ascending: the order of the ragged
+                                    outputs of the compaction calls                     */
+       EA_SLOTS_BY_TOKEN = 1 };  /* sequence after sequence, token after token, the KV heads of a
+                                    token side by side: the order of a projection's output
+                                    [n_tokens, Hkv, d]                                  */
+
+/* Workspace for the calls of this section; max_q as in ea_paged_attention (1 where that is
+ * not called).  HOST-only arithmetic. */
+ea_status ea_paged_workspace_bytes(const ea_paged_shape* shape, int32_t max_q, size_t* out_bytes);
+
+/*
+ * Block tables and slot maps when the lists' lengths change from old_lens to
+ * new_lens.  Lists that grow over a page boundary take pages, in ascending order
+ * of (list, page): first those that shrinking lists give back, last list and
+ * last page first, then the free list from its end.  Surplus released pages are
+ * pushed on the free list.  Hence a shrink that undoes a growth leaves the free
+ * list as it was (proposed tokens that are rejected).
+ *
+ * old_lens, new_lens  int32 [n_seqs, Hkv]
+ * block_table  int32 [n_seqs, Hkv, max_pages], updated: the first
+ *              ceil(old / page_rows) entries of a list are its pages; entries of
+ *              released pages become -1, all others beyond the list stay as they are
+ * free_pages   int32 [n_pages], n_free int32 [1]: the first n_free entries are
+ *              the pages that nobody holds; both updated
+ * slots_opt    int32 [slot_capacity] or NULL: the slots of the rows old .. new - 1 of
+ *              every list that grows, in the given order; -1 behind the last
+ * offsets_opt  NULL, or int32 [n_seqs * Hkv + 1] (by list): where each list's
+ *              slots begin; int32 [n_seqs + 1] (by token): each sequence's first
+ *              token, the q_offsets of ea_paged_attention
+ * All or nothing: when the pool has too few pages, a length is negative or
+ * beyond max_pages * page_rows, the new rows exceed slot_capacity, or (by token) the
+ * heads of a sequence gain different numbers of rows, EA_ERR_PAGES is recorded,
+ * the table and the free list stay as they are, every slot is -1 and every
+ * offset 0.
+ */
+ea_status ea_page_plan(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old_lens,
+                       const int32_t* new_lens, int32_t* block_table, int32_t* free_pages,
+                       int32_t* n_free, int32_t order, int32_t* slots_opt, int32_t slot_capacity,
+                       int32_t* offsets_opt, void* cuda_stream);
+
+/*
+ * The slots of rows first_row .. end_row - 1 of every list (none where end_row <=
+ * first_row), from a table that stands; arguments, order and failures as for
+ * ea_page_plan.  A row on a page number outside the pool gets -1.
+ */
+ea_status ea_page_slots(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* block_table,
+                        const int32_t* first_row, const int32_t* end_row, int32_t order,
+                        int32_t* slots, int32_t slot_capacity, int32_t* offsets_opt,
+                        void* cuda_stream);
+
+/*
+ * Rows into their slots: k_pages[slots[i]] = k_new[i], v_pages[slots[i]] = v_new[i].
+ * slots     int32 [n_rows]; -1: the row goes nowhere; other numbers outside the pool
+ *           are skipped and recorded (EA_ERR_PAGES).  The slots of one call are
+ *           distinct (a plan's always are).
+ * k_new, v_new  bf16 [n_rows, d], 16-byte aligned; row i begins at
+ *           (i / Hkv) * stride + (i % Hkv) * d elements, so that rows by token can be read
+ *           where a fused projection left them; k_stride, v_stride: 0 (dense), or
+ *           a multiple of 8 of at least Hkv * d (n_rows then a multiple of Hkv)
+ * k_pages, v_pages  bf16 [n_pages, page_rows, d], 16-byte aligned
+ *
+ * ea_page_load: the other way, k_out, v_out bf16 [n_rows, d]; rows with slot -1 are
+ * left as they are.
+ */
+ea_status ea_page_store(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* slots,
+                        int64_t n_rows, const void* k_new, const void* v_new, int64_t k_stride,
+                        int64_t v_stride, void* k_pages, void* v_pages, void* cuda_stream);
+ea_status ea_page_load(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* slots,
+                       int64_t n_rows, const void* k_pages, const void* v_pages, void* k_out,
+                       void* v_out, void* cuda_stream);
+
+/*
+ * Attention of the new tokens of every sequence (a chunk of a prompt, one
+ * generated token, or a mix) over the pairs of its lists:
+ *     out[t, h] = sum_p softmax_p(scale * q[t, h] . k_p) v_p,   lse[t, h] = log sum_p exp(scale * q[t, h] . k_p)
+ * over the rows p of list (s, h / G) that token t sees.  The new tokens' own pairs
+ * are the LAST rows of the list (ea_page_store comes first); token i of the m new
+ * ones of a sequence sees, with causal != 0, the rows p <= n - m + i of a list of n
+ * rows (evicted rows left no gap: order is all that counts), with causal = 0 all n.
+ * A token that sees no row gets zeros and lse = -infinity.
+ *
+ * q          bf16 [n_tokens, Hq, d], POST-RoPE, 16-byte aligned; q_stride: elements between
+ *            tokens (0 = dense), a multiple of 8 of at least Hq * d
+ * q_offsets  int32 [n_seqs + 1] DEVICE, ascending: sequence s owns the rows
+ *            q_offsets[s] .. q_offsets[s + 1] - 1 of q; rows outside all sequences are not
+ *            read and their outputs stay as they are
+ * max_q      HOST: the most new tokens of one sequence, <= n_tokens (a sequence that
+ *            has more is recorded as EA_ERR_PAGES, its first max_q tokens are served)
+ * kv_lens    int32 [n_seqs, Hkv] DEVICE: rows of each list, the new tokens' included
+ * block_table, k_pages, v_pages  as above.  Rows behind a list's end may hold anything;
+ *            value rows below it must be finite.  A page number outside the pool
+ *            is recorded and leaves the outputs of its list unspecified.
+ * scale      finite (1/sqrt(d) as a rule)
+ * out        bf16 [n_tokens, Hq, d] dense, 16-byte aligned;  lse_opt fp32 [n_tokens, Hq] or NULL
+ * Scores, softmax and sums are fp32; the weights are rounded to bf16 for the
+ * product with V, whose accumulation is fp32.  Results do not depend on timing.
+ */
+ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape, const void* q,
+                             int64_t q_stride, int32_t n_tokens, const int32_t* q_offsets,
+                             int32_t max_q, const int32_t* kv_lens, const int32_t* block_table,
+                             const void* k_pages, const void* v_pages, float scale, int32_t causal,
+                             void* out, float* lse_opt, void* cuda_stream);
+
+/*
  * Limits the persistent log-score kernel of this context (Eq. 7; one CTA per SM,
  * each taking the SM's whole register file and shared memory) to n_sms SMs,
  * so that work launched beside it - another context's memory-bound passes, a
@@ -563,7 +701,7 @@ ea_status ea_set_side_sms(ea_ctx* ctx, int32_t n_sms);
 
 /*
  * Synchronises cuda_stream and returns the device-side status recorded since
- * the last call of this function (EA_OK, EA_ERR_DEVICE_TIMEOUT, or
+ * the last call of this function (EA_OK, EA_ERR_DEVICE_TIMEOUT, EA_ERR_PAGES, or
  * EA_ERR_CUDA if the stream reports an error), then clears it.
  */
 ea_status ea_sync_status(ea_ctx* ctx, void* cuda_stream);

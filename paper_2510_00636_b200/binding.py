@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libea.so")
 ROPE_HALF_SPLIT, ROPE_INTERLEAVED = 0, 1
 GROUP_MEAN_PROB, GROUP_SUM_PROB, GROUP_MEAN_LOGIT = 0, 1, 2
 COV_POPULATION, COV_SAMPLE = 0, 1
+SLOTS_BY_LIST, SLOTS_BY_TOKEN = 0, 1
 
 EXPORTS = (
     "ea_version", "ea_status_string", "ea_workspace_bytes", "ea_n_kept", "ea_create", "ea_destroy",
@@ -26,6 +27,7 @@ EXPORTS = (
     "ea_profile_end", "ea_host_workspace_bytes", "ea_compress_host", "ea_query_stats_static",
     "ea_select_compact_adaptive", "ea_n_floor", "ea_query_stats_hidden", "ea_wo_gram", "ea_score_wo",
     "ea_select_compact_inplace", "ea_selftest_wait_timeout", "ea_last_cuda_error", "ea_set_sm_budget", "ea_set_side_sms", "ea_set_fused_stats", "ea_cache_append", "ea_window_push", "ea_query_stats_ring", "ea_score_q8", "ea_score_q8_scratch_bytes", "ea_select_compact_q8", "ea_cache_append_q8", "ea_select_compact_inplace_q8", "ea_select_compact_adaptive_q8", "ea_value_norms", "ea_score_vnorm", "ea_carry_f32_inplace", "ea_select_compact_inplace_unordered",
+    "ea_paged_workspace_bytes", "ea_page_plan", "ea_page_slots", "ea_page_store", "ea_page_load", "ea_paged_attention",
 )
 STATIC_MAX_ROPE_PAIRS = 16384
 
@@ -42,6 +44,11 @@ class Shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "n_units", "n_q_heads", "n_kv_heads", "head_dim", "n_keys", "window", "rope_layout",
         "group_mode", "cov_norm", "kv_capacity")]
+
+
+class PagedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_seqs", "n_q_heads", "n_kv_heads", "head_dim", "page_rows", "n_pages", "max_pages")]
 
 
 _lib = None
@@ -106,6 +113,16 @@ def lib() -> ctypes.CDLL:
         L.ea_carry_f32_inplace.argtypes = [vp, sp, vp, i32, vp, vp]
         L.ea_value_norms.restype = L.ea_score_vnorm.restype = L.ea_carry_f32_inplace.restype = ctypes.c_int
         L.ea_score_q8_scratch_bytes.restype = ctypes.c_int
+        psp = ctypes.POINTER(PagedShape)
+        L.ea_paged_workspace_bytes.argtypes = [psp, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.ea_page_plan.argtypes = [vp, psp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp]
+        L.ea_page_slots.argtypes = [vp, psp, vp, vp, vp, i32, vp, i32, vp, vp]
+        L.ea_page_store.argtypes = [vp, psp, vp, i64, vp, vp, i64, i64, vp, vp, vp]
+        L.ea_page_load.argtypes = [vp, psp, vp, i64, vp, vp, vp, vp, vp]
+        L.ea_paged_attention.argtypes = [vp, psp, vp, i64, i32, vp, i32, vp, vp, vp, vp, f32, i32, vp, vp, vp]
+        for name in ("ea_paged_workspace_bytes", "ea_page_plan", "ea_page_slots", "ea_page_store", "ea_page_load",
+                     "ea_paged_attention"):
+            getattr(L, name).restype = ctypes.c_int
         L.ea_set_fused_stats.argtypes = [vp, i32]
         L.ea_set_fused_stats.restype = ctypes.c_int
         L.ea_set_sm_budget.argtypes = [vp, i32]
@@ -632,3 +649,165 @@ def ea_compress_host(ctx: Context, shape: Shape, q_win, k, v, pos_next, n_future
                                   int(n_kept), int(units_per_chunk), _ptr(kept_idx), _ptr(k_out),
                                   _ptr(v_out), _ptr(scores), _stream(ctx.device)), "ea_compress_host")
     return kept_idx, k_out, v_out
+
+
+# ---- paged cache -----------------------------------------------------------------------------------------------------
+def make_paged_shape(n_seqs, n_q_heads, n_kv_heads, head_dim, page_rows, n_pages, max_pages) -> PagedShape:
+    return PagedShape(n_seqs, n_q_heads, n_kv_heads, head_dim, page_rows, n_pages, max_pages)
+
+
+def ea_paged_workspace_bytes(shape: PagedShape, max_q: int = 1) -> int:
+    """Workspace of the paged-cache calls (``max_q``: the most new tokens of one sequence in ``ea_paged_attention``)."""
+    out = ctypes.c_size_t(0)
+    _check(lib().ea_paged_workspace_bytes(ctypes.byref(shape), int(max_q), ctypes.byref(out)), "ea_paged_workspace_bytes")
+    return int(out.value)
+
+
+def _sized(t, dtype, name, *sizes):
+    _dev_tensor(t, dtype, name)
+    if tuple(t.shape) != sizes:
+        raise ValueError(f"{name}: expected shape {list(sizes)}, got {list(t.shape)}")
+    return t
+
+
+def _on_device(ctx, *tensors):
+    for t in tensors:
+        if t is not None and t.device.index != (ctx.device.index or 0):
+            raise ValueError(f"a tensor on {t.device} in a call of a context on {ctx.device}")
+
+
+def _pools(shape, k_pages, v_pages):
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        _sized(t, torch.bfloat16, name, shape.n_pages, shape.page_rows, shape.head_dim)
+
+
+def _slot_outputs(shape, order, n_slots, slots, offsets, device):
+    if slots is None:
+        slots = torch.empty(int(n_slots), dtype=torch.int32, device=device)
+    elif slots.dim() != 1:
+        raise ValueError("slots: expected one dimension")
+    n = (shape.n_seqs if order == SLOTS_BY_TOKEN else shape.n_seqs * shape.n_kv_heads) + 1
+    if offsets is None:
+        offsets = torch.empty(n, dtype=torch.int32, device=device)
+    return _dev_tensor(slots, torch.int32, "slots"), _sized(offsets, torch.int32, "offsets", n)
+
+
+def ea_page_plan(ctx: Context, shape: PagedShape, old_lens, new_lens, block_table, free_pages, n_free, n_slots=None,
+                 order: int = SLOTS_BY_LIST, slots=None, offsets=None):
+    """Takes and gives back pages as the lists' lengths (int32 [S,Hkv]) change; ``block_table`` int32 [S,Hkv,max_pages],
+    ``free_pages`` int32 [n_pages] and ``n_free`` int32 [1] are updated.  With ``n_slots`` (capacity of the slot map) or
+    ``slots`` returns (slots, offsets) of the new rows, else None."""
+    S, Hkv = shape.n_seqs, shape.n_kv_heads
+    _sized(old_lens, torch.int32, "old_lens", S, Hkv)
+    _sized(new_lens, torch.int32, "new_lens", S, Hkv)
+    _sized(block_table, torch.int32, "block_table", S, Hkv, shape.max_pages)
+    _sized(free_pages, torch.int32, "free_pages", shape.n_pages)
+    _sized(n_free, torch.int32, "n_free", 1)
+    want = n_slots is not None or slots is not None
+    if want:
+        slots, offsets = _slot_outputs(shape, order, n_slots, slots, offsets, old_lens.device)
+    elif offsets is not None:
+        raise ValueError("offsets: given without n_slots or slots")
+    _on_device(ctx, old_lens, new_lens, block_table, free_pages, n_free, slots, offsets)
+    _check(lib().ea_page_plan(ctx._h, ctypes.byref(shape), _ptr(old_lens), _ptr(new_lens), _ptr(block_table),
+                              _ptr(free_pages), _ptr(n_free), int(order), _ptr(slots), int(slots.numel()) if want else 0,
+                              _ptr(offsets), _stream(ctx.device)), "ea_page_plan")
+    return (slots, offsets) if want else None
+
+
+def ea_page_slots(ctx: Context, shape: PagedShape, block_table, first_row, end_row, n_slots=None,
+                  order: int = SLOTS_BY_LIST, slots=None, offsets=None):
+    """Slots of the rows ``first_row .. end_row - 1`` (int32 [S,Hkv]) of every list -> (slots [n_slots], offsets)."""
+    S, Hkv = shape.n_seqs, shape.n_kv_heads
+    _sized(block_table, torch.int32, "block_table", S, Hkv, shape.max_pages)
+    _sized(first_row, torch.int32, "first_row", S, Hkv)
+    _sized(end_row, torch.int32, "end_row", S, Hkv)
+    if n_slots is None and slots is None:
+        raise ValueError("ea_page_slots: give n_slots or slots")
+    slots, offsets = _slot_outputs(shape, order, n_slots, slots, offsets, first_row.device)
+    _on_device(ctx, block_table, first_row, end_row, slots, offsets)
+    _check(lib().ea_page_slots(ctx._h, ctypes.byref(shape), _ptr(block_table), _ptr(first_row), _ptr(end_row), int(order),
+                               _ptr(slots), int(slots.numel()), _ptr(offsets), _stream(ctx.device)), "ea_page_slots")
+    return slots, offsets
+
+
+def _token_rows(t, name, heads, d):
+    """(data pointer holder, elements between tokens or 0, rows) of [rows, d] (dense) or [tokens, heads, d] whose tokens
+    may lie apart."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.bfloat16):
+        raise TypeError(f"{name}: expected a CUDA tensor of {torch.bfloat16}")
+    if t.dim() == 2 and t.shape[1] == d and t.is_contiguous():
+        return t, 0, t.shape[0]
+    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, d):
+        raise ValueError(f"{name}: expected [tokens, {heads}, {d}] or dense [rows, {d}], got {list(t.shape)}")
+    if t.is_contiguous():
+        return t, 0, t.shape[0] * heads
+    if t.stride(2) != 1 or t.stride(1) != d:
+        raise ValueError(f"{name}: the heads of a token must lie side by side")
+    if t.shape[0] <= 1:
+        return t, 0, t.shape[0] * heads
+    if t.stride(0) < heads * d or t.stride(0) % 8 != 0:
+        raise ValueError(f"{name}: tokens must not overlap and must lie a multiple of 8 elements apart")
+    return t, t.stride(0), t.shape[0] * heads
+
+
+def ea_page_store(ctx: Context, shape: PagedShape, slots, k_new, v_new, k_pages, v_pages):
+    """Rows ``k_new, v_new`` bf16 ([rows, d], or [tokens, Hkv, d] with tokens any distance apart) into ``slots`` int32 [rows]
+    of ``k_pages, v_pages`` [n_pages, page_rows, d] (in place; -1: the row goes nowhere)."""
+    _pools(shape, k_pages, v_pages)
+    _, ks, n = _token_rows(k_new, "k_new", shape.n_kv_heads, shape.head_dim)
+    _, vs, nv = _token_rows(v_new, "v_new", shape.n_kv_heads, shape.head_dim)
+    if n != nv:
+        raise ValueError("k_new and v_new differ in rows")
+    _sized(slots, torch.int32, "slots", n)
+    _on_device(ctx, slots, k_new, v_new, k_pages, v_pages)
+    _check(lib().ea_page_store(ctx._h, ctypes.byref(shape), _ptr(slots), n, _ptr(k_new), _ptr(v_new), ks, vs, _ptr(k_pages),
+                               _ptr(v_pages), _stream(ctx.device)), "ea_page_store")
+
+
+def ea_page_load(ctx: Context, shape: PagedShape, slots, k_pages, v_pages, k_out=None, v_out=None):
+    """Rows out of ``slots`` int32 [rows] -> (k, v) bf16 [rows, d]; rows with slot -1 are left as they are."""
+    _dev_tensor(slots, torch.int32, "slots")
+    _pools(shape, k_pages, v_pages)
+    n, d = slots.numel(), shape.head_dim
+    if k_out is None:
+        k_out = torch.empty((n, d), dtype=torch.bfloat16, device=slots.device)
+    if v_out is None:
+        v_out = torch.empty((n, d), dtype=torch.bfloat16, device=slots.device)
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        _dev_tensor(t, torch.bfloat16, name)
+        if t.numel() != n * d:
+            raise ValueError(f"{name}: expected {n} rows of {d}")
+    _on_device(ctx, slots, k_pages, v_pages, k_out, v_out)
+    _check(lib().ea_page_load(ctx._h, ctypes.byref(shape), _ptr(slots), n, _ptr(k_pages), _ptr(v_pages), _ptr(k_out),
+                              _ptr(v_out), _stream(ctx.device)), "ea_page_load")
+    return k_out, v_out
+
+
+def ea_paged_attention(ctx: Context, shape: PagedShape, q, q_offsets, max_q: int, kv_lens, block_table, k_pages, v_pages,
+                       scale: float | None = None, causal: bool = True, out=None, lse=None, want_lse: bool = False):
+    """Attention of new tokens ``q`` bf16 [T,Hq,d] (tokens any distance apart; sequence s owns ``q_offsets[s] ..
+    q_offsets[s+1]``, int32 [S+1], at most ``max_q`` tokens each) over the lists of ``kv_lens`` int32 [S,Hkv] rows ->
+    out bf16 [T,Hq,d] (and lse fp32 [T,Hq] if asked).  The new tokens' own pairs are the last rows of the lists."""
+    S, Hq, Hkv, d = shape.n_seqs, shape.n_q_heads, shape.n_kv_heads, shape.head_dim
+    if not (isinstance(q, torch.Tensor) and q.dim() == 3):
+        raise ValueError(f"q: expected [tokens, {Hq}, {d}]")
+    _, stride, rows = _token_rows(q, "q", Hq, d)
+    T = q.shape[0]
+    _sized(q_offsets, torch.int32, "q_offsets", S + 1)
+    _sized(kv_lens, torch.int32, "kv_lens", S, Hkv)
+    _sized(block_table, torch.int32, "block_table", S, Hkv, shape.max_pages)
+    _pools(shape, k_pages, v_pages)
+    if out is None:
+        out = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+    _sized(out, torch.bfloat16, "out", T, Hq, d)
+    if lse is not None:
+        _sized(lse, torch.float32, "lse", T, Hq)
+    _on_device(ctx, q, q_offsets, kv_lens, block_table, k_pages, v_pages, out, lse)
+    _check(lib().ea_paged_attention(ctx._h, ctypes.byref(shape), _ptr(q), stride, T, _ptr(q_offsets), int(max_q),
+                                    _ptr(kv_lens), _ptr(block_table), _ptr(k_pages), _ptr(v_pages),
+                                    float(d ** -0.5 if scale is None else scale), int(bool(causal)), _ptr(out), _ptr(lse),
+                                    _stream(ctx.device)), "ea_paged_attention")
+    return (out, lse) if lse is not None else out

@@ -89,6 +89,7 @@ const char* ea_status_string(ea_status s) {
         case EA_ERR_CUDA: return "EA_ERR_CUDA";
         case EA_ERR_NOT_SM100: return "EA_ERR_NOT_SM100";
         case EA_ERR_DEVICE_TIMEOUT: return "EA_ERR_DEVICE_TIMEOUT";
+        case EA_ERR_PAGES: return "EA_ERR_PAGES";
     }
     return "EA_ERR_UNKNOWN";
 }
@@ -143,9 +144,9 @@ ea_status ea_create(ea_ctx** out_ctx, int device, size_t workspace_bytes) {
     ctx->ev_stop = new (std::nothrow) cudaEvent_t[kMaxProfileEvents];
     bool ok = ctx->ev_start && ctx->ev_stop;
     if (ok && workspace_bytes > 0) ok = cudaMalloc(&ctx->workspace, workspace_bytes) == cudaSuccess;
-    if (ok) ok = cudaHostAlloc((void**)&ctx->status_host, sizeof(int), cudaHostAllocMapped) == cudaSuccess;
+    if (ok) ok = cudaHostAlloc((void**)&ctx->status_host, 2 * sizeof(int), cudaHostAllocMapped) == cudaSuccess;
     if (ok) {
-        *ctx->status_host = 0;
+        ctx->status_host[0] = ctx->status_host[1] = 0;
         ok = cudaHostGetDevicePointer((void**)&ctx->status_dev, ctx->status_host, 0) == cudaSuccess;
     }
     if (!ok) {
@@ -639,8 +640,8 @@ ea_status ea_set_side_sms(ea_ctx* ctx, int32_t n_sms) {
 ea_status ea_sync_status(ea_ctx* ctx, void* cuda_stream) {
     if (!ctx) return EA_ERR_INVALID_ARG;
     EA_CUDA_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)));
-    const int s = *ctx->status_host;
-    *ctx->status_host = 0;
+    const int s = ctx->status_host[0] ? ctx->status_host[0] : ctx->status_host[1];
+    ctx->status_host[0] = ctx->status_host[1] = 0;
     return s == 0 ? EA_OK : static_cast<ea_status>(s);
 }
 

@@ -23,7 +23,8 @@ struct ea_ctx {
     cudaEvent_t ev_fork, ev_join;
     void* workspace;
     size_t workspace_bytes;
-    int* status_host;    // pinned, mapped: device kernels write EA_ERR_DEVICE_TIMEOUT here
+    int* status_host;    // two pinned, mapped words: [0] device kernels write EA_ERR_DEVICE_TIMEOUT (other waits
+                         // give up when they see it), [1] the paged-cache calls write EA_ERR_PAGES
     int* status_dev;     // device alias of status_host
     // benchmark instrumentation (ea_profile_begin / ea_profile_end)
     bool profiling;

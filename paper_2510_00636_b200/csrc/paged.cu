@@ -1,0 +1,502 @@
+// The paged cache: pages taken and given back as lists grow and shrink, slot maps, and rows moved into and out
+// of their slots.  (The attention that reads the cache is in paged_attn.cu.)
+//
+// A list is the cache of one (sequence, KV head).  With have = ceil(old / P) and want = ceil(new / P) pages of P
+// rows, the lists that grow take N = sum max(0, want - have) pages, those that shrink give M back.  Both sides are
+// numbered, takes in ascending order of (list, page), releases in descending order, and item t < max(N, M) is one
+// page that changes hands:
+//     page(t)  = t < M ? the t-th released page : free[top - 1 - (t - M)]
+//     t < N    : page(t) becomes the table entry of the t-th take
+//     N <= t   : page(t) is pushed, free[top + t - N]
+// So the free list is either only read or only written, every entry of the table has one writer, and no order
+// between threads matters.  A shrink that undoes a growth leaves the free list as it was.
+#include "paged.h"
+#include "ptx_sm100.cuh"
+
+namespace {
+
+constexpr int kSelfScanLists = 4096;      // up to here every CTA scans the lengths itself (48 KiB of prefixes)
+constexpr int kOneCtaSlots = 8192;        // up to here a plan is one CTA's work
+constexpr int kClusterSlots = 65536;      // up to here it is one cluster's (one launch); beyond, three launches over all SMs
+constexpr int kScanThreads = 1024, kMoveThreads = 256;
+
+struct PlanArgs {
+    const int32_t* old_lens;     // first rows (slots only)
+    const int32_t* new_lens;     // end rows
+    int32_t* table;
+    int32_t* free_pages;         // nullptr: the tables stand (ea_page_slots)
+    int32_t* n_free;
+    int32_t* slots;
+    int32_t* offsets;
+    int32_t* scratch;            // prefixes of more than kSelfScanLists lists, and the totals
+    int* status;                 // [1]: page status word
+    int lists, Hkv, shift, n_pages, max_pages, by_token, slot_capacity;
+};
+
+// What a scan finds.  All-or-nothing: a call that cannot be served has n_take = n_give = rows = 0.
+struct Totals {
+    int n_take, n_give, rows, top, bad;
+};
+
+__device__ __forceinline__ int pages_of(int rows, int shift) { return (int)(((unsigned)rows + (1u << shift) - 1u) >> shift); }
+
+struct Tally {
+    long long take, give, rows;
+    int bad;
+};
+
+__device__ __forceinline__ void count_list(const PlanArgs& a, int r, Tally& t) {
+    const int o = a.old_lens[r], n = a.new_lens[r];
+    const long long cap = (long long)a.max_pages << a.shift;
+    if (o < 0 || n < 0 || o > cap || n > cap) {
+        t.bad = 1;
+        return;
+    }
+    const int have = pages_of(o, a.shift), want = pages_of(n, a.shift);
+    t.take += want > have ? want - have : 0;
+    t.give += have > want ? have - want : 0;
+    t.rows += n > o ? n - o : 0;
+    // token order puts the heads of a token side by side: they must gain the same rows
+    if (a.by_token && r % a.Hkv != 0) {
+        const int o0 = a.old_lens[r - r % a.Hkv], n0 = a.new_lens[r - r % a.Hkv];
+        if ((n > o ? n - o : 0) != (n0 > o0 ? n0 - o0 : 0)) t.bad = 1;
+    }
+}
+
+__device__ __forceinline__ long long shfl_up_ll(long long v, int d) { return __shfl_up_sync(0xffffffffu, v, d); }
+
+// Exclusive prefixes of pages taken, pages given back and rows gained, over all lists, into take / give / rows
+// (lists + 1 entries each; shared or global memory).  Every thread of the CTA calls it; the totals are returned
+// to all of them.  Entries hold 32 bits: totals beyond that are refused.
+template <int THREADS>
+__device__ Totals scan_lists(const PlanArgs& a, int32_t* take, int32_t* give, int32_t* rows) {
+    __shared__ Tally warp_sum[THREADS / 32];
+    __shared__ Totals total;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.lists + THREADS - 1) / THREADS;
+    const int r0 = min(a.lists, tid * per), r1 = min(a.lists, r0 + per);
+    Tally mine = {0, 0, 0, 0};
+    for (int r = r0; r < r1; ++r) count_list(a, r, mine);
+    Tally inc = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long x = shfl_up_ll(inc.take, d), y = shfl_up_ll(inc.give, d), z = shfl_up_ll(inc.rows, d);
+        if (lane >= d) {
+            inc.take += x;
+            inc.give += y;
+            inc.rows += z;
+        }
+    }
+    const int any_bad = __any_sync(0xffffffffu, mine.bad);
+    if (lane == 31) warp_sum[warp] = {inc.take, inc.give, inc.rows, any_bad};
+    __syncthreads();
+    long long bt = 0, bg = 0, br = 0, tt = 0, tg = 0, tr = 0;
+    int bad = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w == warp) {
+            bt = tt;
+            bg = tg;
+            br = tr;
+        }
+        tt += warp_sum[w].take;
+        tg += warp_sum[w].give;
+        tr += warp_sum[w].rows;
+        bad |= warp_sum[w].bad;
+    }
+    if (tid == 0) {
+        int top = 0;
+        if (a.free_pages) {
+            top = *a.n_free;
+            if (top < 0 || top > a.n_pages || tt - tg > top || top + tg - tt > a.n_pages || tt > a.n_pages || tg > a.n_pages) bad = 1;
+        }
+        if (tr > 0x7fffffffLL) bad = 1;
+        if (a.slots && tr > a.slot_capacity) bad = 1;
+        total = bad ? Totals{0, 0, 0, top, 1} : Totals{(int)tt, (int)tg, (int)tr, top, 0};
+    }
+    __syncthreads();
+    const Totals out = total;
+    long long t = bt + inc.take - mine.take, g = bg + inc.give - mine.give, n = br + inc.rows - mine.rows;
+    for (int r = r0; r < r1; ++r) {
+        take[r] = out.bad ? 0 : (int)t;
+        give[r] = out.bad ? 0 : (int)g;
+        rows[r] = out.bad ? 0 : (int)n;
+        Tally one = {0, 0, 0, 0};
+        count_list(a, r, one);
+        t += one.take;
+        g += one.give;
+        n += one.rows;
+    }
+    if (tid == 0) {
+        take[a.lists] = out.n_take;
+        give[a.lists] = out.n_give;
+        rows[a.lists] = out.rows;
+    }
+    __syncthreads();
+    return out;
+}
+
+// last r with prefix[r] <= x (x < prefix[lists])
+__device__ __forceinline__ int find_list(const int32_t* prefix, int lists, int x) {
+    int lo = 0, hi = lists;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (prefix[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Items t0, t0 + step, ... of the pages that change hands.
+__device__ void move_pages(const PlanArgs& a, const Totals& tot, const int32_t* take, const int32_t* give, int t0, int step) {
+    const int items = max(tot.n_take, tot.n_give);
+    for (int t = t0; t < items; t += step) {
+        int page;
+        if (t < tot.n_give) {
+            const int x = tot.n_give - 1 - t;                       // last list first, last page first
+            const int r = find_list(give, a.lists, x);
+            int32_t* entry = a.table + (size_t)r * a.max_pages + pages_of(a.new_lens[r], a.shift) + (x - give[r]);
+            page = *entry;
+            *entry = -1;
+        } else {
+            page = a.free_pages[tot.top - 1 - (t - tot.n_give)];
+        }
+        if (t < tot.n_take) {
+            const int r = find_list(take, a.lists, t);
+            a.table[(size_t)r * a.max_pages + pages_of(a.old_lens[r], a.shift) + (t - take[r])] = page;
+        } else {
+            a.free_pages[tot.top + t - tot.n_take] = page;
+        }
+    }
+}
+
+__device__ __forceinline__ int slot_of(const PlanArgs& a, int r, int p) {
+    const int page = a.table[(size_t)r * a.max_pages + (p >> a.shift)];
+    return (unsigned)page < (unsigned)a.n_pages ? (page << a.shift) + (p & ((1 << a.shift) - 1)) : -1;
+}
+
+// Slots 4 t .. 4 t + 3 for t = t0, t0 + step, ...: rows old .. new of every list, -1 behind the last.
+__device__ void write_slots(const PlanArgs& a, const Totals& tot, const int32_t* rows, long long t0, long long step) {
+    const bool wide = (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
+    for (long long q = t0; q * 4 < a.slot_capacity; q += step) {
+        int v[4];
+        int r = -1, next = 0;                                        // list order: the list of the last slot, and where it ends
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const long long t = q * 4 + e;
+            v[e] = -1;
+            if (t >= tot.rows) continue;
+            if (a.by_token) {
+                // rows[] counts Hkv rows per token: token t / Hkv begins its sequence at rows[s * Hkv] / Hkv
+                const int token = (int)(t / a.Hkv), g = (int)(t % a.Hkv);
+                const int s = find_list(rows, a.lists, token * a.Hkv) / a.Hkv;      // lists of a sequence gain alike
+                const int list = s * a.Hkv + g;
+                v[e] = slot_of(a, list, a.old_lens[list] + token - rows[s * a.Hkv] / a.Hkv);
+            } else {
+                if (r < 0 || t >= next) {
+                    r = find_list(rows, a.lists, (int)t);
+                    next = rows[r + 1];
+                }
+                v[e] = slot_of(a, r, a.old_lens[r] + (int)t - rows[r]);
+            }
+        }
+        if (wide && q * 4 + 4 <= a.slot_capacity) {
+            reinterpret_cast<int4*>(a.slots)[q] = make_int4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (q * 4 + e < a.slot_capacity) a.slots[q * 4 + e] = v[e];
+        }
+    }
+}
+
+// Offsets (list order: lists + 1 row offsets; token order: sequences + 1 token offsets), the free count, the status.
+__device__ void write_offsets(const PlanArgs& a, const Totals& tot, const int32_t* rows) {
+    if (a.offsets) {
+        const int n = a.by_token ? a.lists / a.Hkv : a.lists;
+        for (int i = threadIdx.x; i <= n; i += blockDim.x) a.offsets[i] = a.by_token ? rows[i * a.Hkv] / a.Hkv : rows[i];
+    }
+    if (threadIdx.x == 0) {
+        if (a.free_pages && !tot.bad) *a.n_free = tot.top - tot.n_take + tot.n_give;
+        if (tot.bad) a.status[1] = (int)EA_ERR_PAGES;
+    }
+}
+
+// The whole plan in one cluster (one launch): for a generation step further launches would cost more than the work.
+// Every CTA scans the lengths for itself; the free count is read before the first cluster barrier and written after
+// the last.
+__global__ void __launch_bounds__(kScanThreads) page_plan_cluster_kernel(const PlanArgs a) {
+    extern __shared__ int32_t prefix[];
+    int32_t *take = prefix, *give = take + a.lists + 1, *rows = give + a.lists + 1;
+    const Totals tot = scan_lists<kScanThreads>(a, take, give, rows);
+    const int t0 = blockIdx.x * kScanThreads + threadIdx.x, step = gridDim.x * kScanThreads;
+    ptx::cluster_sync();
+    if (a.free_pages) {
+        move_pages(a, tot, take, give, t0, step);
+        ptx::cluster_sync();                                        // the slots read the entries just written
+    }
+    if (a.slots) write_slots(a, tot, rows, t0, step);
+    if (blockIdx.x == 0) write_offsets(a, tot, rows);
+}
+
+// Larger plans: prefixes and totals into the workspace, then the pages, then the slots.
+__global__ void __launch_bounds__(kScanThreads) page_scan_kernel(const PlanArgs a) {
+    int32_t *take = a.scratch, *give = take + a.lists + 1, *rows = give + a.lists + 1;
+    const Totals tot = scan_lists<kScanThreads>(a, take, give, rows);
+    if (threadIdx.x == 0) *reinterpret_cast<Totals*>(rows + a.lists + 1) = tot;
+    write_offsets(a, tot, rows);
+}
+
+__global__ void __launch_bounds__(kMoveThreads) page_move_kernel(const PlanArgs a) {
+    const int32_t *take = a.scratch, *give = take + a.lists + 1;
+    const Totals tot = *reinterpret_cast<const Totals*>(give + 2 * (a.lists + 1));
+    move_pages(a, tot, take, give, blockIdx.x * kMoveThreads + threadIdx.x, gridDim.x * kMoveThreads);
+}
+
+// SCAN: the tables stand and the lists are few: every CTA scans the lengths for itself, and one launch is all.
+template <bool SCAN>
+__global__ void __launch_bounds__(kMoveThreads) page_slots_kernel(const PlanArgs a) {
+    extern __shared__ int32_t prefix[];
+    const int32_t* rows;
+    Totals tot;
+    if (SCAN) {
+        rows = prefix + 2 * (a.lists + 1);
+        tot = scan_lists<kMoveThreads>(a, prefix, prefix + a.lists + 1, prefix + 2 * (a.lists + 1));
+        if (blockIdx.x == 0) write_offsets(a, tot, rows);
+    } else {
+        rows = a.scratch + 2 * (a.lists + 1);
+        tot = *reinterpret_cast<const Totals*>(rows + a.lists + 1);
+    }
+    if (a.slots) write_slots(a, tot, rows, (long long)blockIdx.x * kMoveThreads + threadIdx.x, (long long)gridDim.x * kMoveThreads);
+}
+
+// rows <-> slots, 16 bytes of K and of V per thread and step.  A slot of -1 names no row; any other number outside the
+// pool is reported and skipped.  src: row i of the rows side begins at (i / group) * group_stride + (i % group) * d
+// elements (dense rows: group = 1, group_stride = d).
+template <bool STORE, int LPR /* 16-byte pieces per row */>
+__global__ void __launch_bounds__(256) page_rows_kernel(const int32_t* __restrict__ slots, long long n_rows, uint4* __restrict__ k_rows,
+                                                        uint4* __restrict__ v_rows, int group, long long k_stride, long long v_stride,
+                                                        uint4* __restrict__ k_pages, uint4* __restrict__ v_pages, int n_slots, int* status) {
+    constexpr int U = 4;                       // rows in flight per thread: eight 16-byte loads hide the latency
+    constexpr int ROWS = 256 / LPR;            // rows of one step of the CTA
+    const int piece = threadIdx.x % LPR;
+    const long long step = (long long)gridDim.x * ROWS * U;
+    for (long long r0 = (long long)blockIdx.x * ROWS * U + threadIdx.x / LPR; r0 < n_rows; r0 += step) {
+        uint4 k[U], v[U];
+        int slot[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * ROWS;
+            slot[u] = r < n_rows ? __ldg(slots + r) : -1;
+            if (slot[u] >= n_slots || slot[u] < -1) {
+                status[1] = (int)EA_ERR_PAGES;
+                slot[u] = -1;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * ROWS;
+            if (slot[u] < 0) continue;
+            if (STORE) {
+                const long long gi = group == 1 ? r : r / group, ge = group == 1 ? 0 : (r % group) * LPR;
+                k[u] = __ldcs(k_rows + gi * k_stride + ge + piece);
+                v[u] = __ldcs(v_rows + gi * v_stride + ge + piece);
+            } else {
+                k[u] = __ldcs(k_pages + (long long)slot[u] * LPR + piece);
+                v[u] = __ldcs(v_pages + (long long)slot[u] * LPR + piece);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * ROWS;
+            if (slot[u] < 0) continue;
+            if (STORE) {
+                k_pages[(long long)slot[u] * LPR + piece] = k[u];
+                v_pages[(long long)slot[u] * LPR + piece] = v[u];
+            } else {
+                k_rows[r * LPR + piece] = k[u];
+                v_rows[r * LPR + piece] = v[u];
+            }
+        }
+    }
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+size_t scan_bytes(const ea_paged_shape& s) { return (3 * ((size_t)s.n_seqs * s.n_kv_heads + 1) + sizeof(Totals) / 4) * 4; }
+
+// Lists up to kSelfScanLists need no scratch when one launch does it all, but whether it does depends on the call.
+ea_status launch_plan(const ea_ctx* ctx, PlanArgs a, cudaStream_t st) {
+    const int smem = 3 * (a.lists + 1) * 4;
+    const bool few = a.lists <= kSelfScanLists;
+    const bool resize = a.free_pages != nullptr;
+    const long long quads = ((long long)a.slot_capacity + 3) / 4;
+    const long long want = (quads + kMoveThreads - 1) / kMoveThreads, cap = (long long)ctx->sm_count * 4;
+    const unsigned slot_grid = (unsigned)(want < 1 ? 1 : want < cap ? want : cap);
+    if (few && !resize) {
+        EA_CUDA_TRY(cudaFuncSetAttribute(page_slots_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        page_slots_kernel<true><<<slot_grid, kMoveThreads, smem, st>>>(a);
+        ea_count_launches(ctx, 1);
+        return EA_CHECK_LAUNCH();
+    }
+    if (few && a.slot_capacity <= kClusterSlots) {
+        EA_CUDA_TRY(cudaFuncSetAttribute(page_plan_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        // without slots nothing bounds the pages that move but the pool, so that form gets the wide cluster
+        const unsigned ctas = a.slots && a.slot_capacity <= kOneCtaSlots ? 1 : 8;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(ctas);
+        cfg.blockDim = dim3(kScanThreads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = ctas;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        EA_CUDA_TRY(cudaLaunchKernelEx(&cfg, page_plan_cluster_kernel, a));
+        ea_count_launches(ctx, 1);
+        return EA_CHECK_LAUNCH();
+    }
+    page_scan_kernel<<<1, kScanThreads, 0, st>>>(a);
+    if (resize) {
+        const long long pages = (a.n_pages + kMoveThreads - 1) / kMoveThreads, most = (long long)ctx->sm_count * 4;
+        page_move_kernel<<<(unsigned)(pages < 1 ? 1 : pages < most ? pages : most), kMoveThreads, 0, st>>>(a);
+    }
+    if (a.slots) page_slots_kernel<false><<<slot_grid, kMoveThreads, 0, st>>>(a);
+    ea_count_launches(ctx, 1 + (resize ? 1 : 0) + (a.slots ? 1 : 0));
+    return EA_CHECK_LAUNCH();
+}
+
+ea_status plan_call(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old_lens, const int32_t* new_lens, int32_t* table,
+                    int32_t* free_pages, int32_t* n_free, bool resize, int32_t order, int32_t* slots, int32_t slot_capacity,
+                    int32_t* offsets, void* cuda_stream) {
+    if (!ctx) return EA_ERR_INVALID_ARG;
+    ea_status st = ea_check_paged_shape(shape);
+    if (st != EA_OK) return st;
+    if (order != EA_SLOTS_BY_LIST && order != EA_SLOTS_BY_TOKEN) return EA_ERR_INVALID_ARG;
+    if (slot_capacity < 0 || (slot_capacity > 0 && !slots)) return EA_ERR_INVALID_ARG;
+    const long long lists = (long long)shape->n_seqs * shape->n_kv_heads;
+    if (lists > 0 && (!old_lens || !new_lens || (shape->max_pages > 0 && !table))) return EA_ERR_INVALID_ARG;
+    if (resize && (!n_free || (shape->n_pages > 0 && !free_pages))) return EA_ERR_INVALID_ARG;
+    if (!aligned4(old_lens) || !aligned4(new_lens) || !aligned4(table) || !aligned4(free_pages) || !aligned4(n_free) ||
+        !aligned4(slots) || !aligned4(offsets))
+        return EA_ERR_INVALID_ARG;
+    if (ctx->workspace_bytes < scan_bytes(*shape)) return EA_ERR_WORKSPACE;
+    if (lists == 0 && slot_capacity == 0 && !offsets) return EA_OK;
+    PlanArgs a = {};
+    a.old_lens = old_lens;
+    a.new_lens = new_lens;
+    a.table = table;
+    a.free_pages = resize ? (free_pages ? free_pages : n_free) : nullptr;      // an empty pool is never indexed
+    a.n_free = n_free;
+    a.slots = slots;
+    a.offsets = offsets;
+    a.scratch = static_cast<int32_t*>(ctx->workspace);
+    a.status = ctx->status_dev;
+    a.lists = (int)lists;
+    a.Hkv = shape->n_kv_heads;
+    a.shift = __builtin_ctz((unsigned)shape->page_rows);
+    a.n_pages = shape->n_pages;
+    a.max_pages = shape->max_pages;
+    a.by_token = order == EA_SLOTS_BY_TOKEN;
+    a.slot_capacity = slot_capacity;
+    int prev = 0;
+    EA_CUDA_TRY(cudaGetDevice(&prev));
+    if (prev != ctx->device) EA_CUDA_TRY(cudaSetDevice(ctx->device));
+    ctx->image_ready = false;                       // the scratch lies where fused statistics keep their images
+    st = launch_plan(ctx, a, static_cast<cudaStream_t>(cuda_stream));
+    if (prev != ctx->device) cudaSetDevice(prev);
+    return st;
+}
+
+template <bool STORE>
+ea_status rows_call(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* slots, int64_t n_rows, void* k_rows, void* v_rows,
+                    int64_t k_stride, int64_t v_stride, void* k_pages, void* v_pages, void* cuda_stream) {
+    if (!ctx) return EA_ERR_INVALID_ARG;
+    ea_status st = ea_check_paged_shape(shape);
+    if (st != EA_OK) return st;
+    if (n_rows < 0 || n_rows > 0x7fffffffLL) return EA_ERR_INVALID_ARG;
+    const int d = shape->head_dim, lpr = d / 8;
+    const int64_t dense = (int64_t)shape->n_kv_heads * d;
+    const bool strided = STORE && (k_stride != 0 || v_stride != 0);
+    if (STORE) {
+        // strides: elements between groups of n_kv_heads rows (the tokens of a fused projection), 0 = dense
+        if (k_stride < 0 || v_stride < 0 || k_stride % 8 != 0 || v_stride % 8 != 0) return EA_ERR_INVALID_ARG;
+        if ((k_stride != 0 && k_stride < dense) || (v_stride != 0 && v_stride < dense)) return EA_ERR_INVALID_ARG;
+        if (strided && n_rows % shape->n_kv_heads != 0) return EA_ERR_INVALID_ARG;
+    }
+    if (n_rows == 0) return EA_OK;
+    if (!slots || !k_rows || !v_rows || (shape->n_pages > 0 && (!k_pages || !v_pages))) return EA_ERR_INVALID_ARG;
+    if (!aligned4(slots) || !aligned16(k_rows) || !aligned16(v_rows) || !aligned16(k_pages) || !aligned16(v_pages)) return EA_ERR_INVALID_ARG;
+    int prev = 0;
+    EA_CUDA_TRY(cudaGetDevice(&prev));
+    if (prev != ctx->device) EA_CUDA_TRY(cudaSetDevice(ctx->device));
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const int group = strided ? shape->n_kv_heads : 1;
+    const long long ks = strided ? (k_stride ? k_stride : dense) / 8 : lpr, vs = strided ? (v_stride ? v_stride : dense) / 8 : lpr;
+    const long long per = 256 / lpr * 4, want = (n_rows + per - 1) / per, cap = (long long)ctx->sm_count * 8;
+    const unsigned grid = (unsigned)(want < cap ? want : cap);
+    const int n_slots = shape->n_pages * shape->page_rows;
+    auto kernel = lpr == 8 ? page_rows_kernel<STORE, 8> : lpr == 16 ? page_rows_kernel<STORE, 16> : page_rows_kernel<STORE, 32>;
+    kernel<<<grid, 256, 0, stream>>>(slots, n_rows, static_cast<uint4*>(k_rows), static_cast<uint4*>(v_rows), group, ks, vs,
+                                     static_cast<uint4*>(k_pages), static_cast<uint4*>(v_pages), n_slots, ctx->status_dev);
+    ea_count_launches(ctx, 1);
+    st = EA_CHECK_LAUNCH();
+    if (prev != ctx->device) cudaSetDevice(prev);
+    return st;
+}
+
+}  // namespace
+
+ea_status ea_check_paged_shape(const ea_paged_shape* s) {
+    if (!s) return EA_ERR_INVALID_ARG;
+    if (s->n_seqs < 0 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->n_pages < 0 || s->max_pages < 0) return EA_ERR_INVALID_ARG;
+    if (s->n_q_heads % s->n_kv_heads != 0) return EA_ERR_INVALID_ARG;
+    if (s->head_dim != 64 && s->head_dim != 128 && s->head_dim != 256) return EA_ERR_UNSUPPORTED;
+    if (s->page_rows != 16 && s->page_rows != 32 && s->page_rows != 64 && s->page_rows != 128) return EA_ERR_UNSUPPORTED;
+    if ((long long)s->n_seqs * s->n_kv_heads > 65535LL) return EA_ERR_UNSUPPORTED;
+    // slot numbers and list lengths are 32-bit
+    if ((long long)s->n_pages * s->page_rows > 0x7fffffffLL || (long long)s->max_pages * s->page_rows > 0x7fffffffLL) return EA_ERR_UNSUPPORTED;
+    return EA_OK;
+}
+
+extern "C" {
+
+ea_status ea_paged_workspace_bytes(const ea_paged_shape* shape, int32_t max_q, size_t* out_bytes) {
+    if (!out_bytes || max_q < 0) return EA_ERR_INVALID_ARG;
+    ea_status st = ea_check_paged_shape(shape);
+    if (st != EA_OK) return st;
+    const size_t scan = scan_bytes(*shape), attn = ea_paged_attn_ws_bytes(*shape, max_q);
+    *out_bytes = ea_align_up(scan > attn ? scan : attn, 256);
+    return EA_OK;
+}
+
+ea_status ea_page_plan(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old_lens, const int32_t* new_lens,
+                       int32_t* block_table, int32_t* free_pages, int32_t* n_free, int32_t order, int32_t* slots_opt,
+                       int32_t slot_capacity, int32_t* offsets_opt, void* cuda_stream) {
+    return plan_call(ctx, shape, old_lens, new_lens, block_table, free_pages, n_free, true, order, slots_opt, slot_capacity,
+                     offsets_opt, cuda_stream);
+}
+
+ea_status ea_page_slots(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* block_table, const int32_t* first_row,
+                        const int32_t* end_row, int32_t order, int32_t* slots, int32_t slot_capacity, int32_t* offsets_opt,
+                        void* cuda_stream) {
+    return plan_call(ctx, shape, first_row, end_row, const_cast<int32_t*>(block_table), nullptr, nullptr, false, order, slots,
+                     slot_capacity, offsets_opt, cuda_stream);
+}
+
+ea_status ea_page_store(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* slots, int64_t n_rows, const void* k_new,
+                        const void* v_new, int64_t k_stride, int64_t v_stride, void* k_pages, void* v_pages, void* cuda_stream) {
+    return rows_call<true>(ctx, shape, slots, n_rows, const_cast<void*>(k_new), const_cast<void*>(v_new), k_stride, v_stride,
+                           k_pages, v_pages, cuda_stream);
+}
+
+ea_status ea_page_load(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* slots, int64_t n_rows, const void* k_pages,
+                       const void* v_pages, void* k_out, void* v_out, void* cuda_stream) {
+    return rows_call<false>(ctx, shape, slots, n_rows, k_out, v_out, 0, 0, const_cast<void*>(k_pages), const_cast<void*>(v_pages),
+                            cuda_stream);
+}
+
+}  // extern "C"

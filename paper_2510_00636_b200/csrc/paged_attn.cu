@@ -1,0 +1,481 @@
+// Attention of new tokens over the paged cache.
+//
+//   x_{h,i,p} = scale * q_{h,i} . k_{g,p}    for the visible rows p of list g = h / G
+//   o_{h,i}   = sum_p e^{x_p - lse} v_{g,p},   lse = log sum_p e^{x_p}
+//
+// The G query heads that share a list and the new tokens of a sequence are packed into rows, row = token * G + head,
+// so that every K/V row is read once for all of them.
+#include "paged.h"
+#include "paged_attn.cuh"
+#include "ptx_sm100.cuh"
+
+using namespace ptx;
+
+namespace {
+
+// ---------------------------------------------------------------------------------------- few rows
+// Row tiles of 16: a generation step has G rows per list, and the time is that of reading K and V once.  One CTA per SM
+// takes an equal, contiguous share of all key blocks of the call, whatever list they belong to (lengths differ by list);
+// a list that several CTAs share leaves partial results (maximum, sum, unnormalised output) for paged_combine_kernel.
+//
+// Inside a CTA one warp keeps TMA boxes of K and V (128-byte swizzle) flowing into a ring, and each of NW warps owns 16
+// keys of every block: scores (mma.sync m16n8k16, 16 rows are one tile), softmax with its own running maximum, and
+// the product with its 16 value rows.  No barrier among the warps until the list ends, where they are merged in a fixed
+// order.  At most 16 of the 128 rows of a tcgen05 tile would be in use here, and the limit is memory.
+template <int D> struct Few {
+    static constexpr int NW = D == 64 ? 8 : 4;
+    static constexpr int BK = NW * 16;                       // keys per block
+    static constexpr int CHUNKS = D / 64;
+    static constexpr int CHUNK_BYTES = BK * 128;             // 64 channels of a block
+    static constexpr int STAGE = 2 * CHUNKS * CHUNK_BYTES;
+    static constexpr int NST = 196608 / STAGE;               // 192 KiB in flight
+    static constexpr int MERGE = NW / 2 * 16 * D * 4;
+    static constexpr int THREADS = NW * 32 + 32;
+    // behind the ring and the merge buffer: barriers, abort flag, range, and [NW][16] maxima and sums
+    static constexpr int TAIL_ML = 16 * NST + 64;
+    static constexpr int TAIL = TAIL_ML + NW * 16 * 8;
+    static constexpr int SMEM = 1024 /* alignment */ + NST * STAGE + MERGE + TAIL;
+    static_assert(SMEM + 1024 <= 232448, "a CTA's shared memory, with room for static arrays");
+};
+
+template <int D>
+__global__ void __launch_bounds__(Few<D>::THREADS, 1)
+paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
+    using C = Few<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+    float* merge = reinterpret_cast<float*>(gen + C::NST * C::STAGE);
+    uint8_t* tail = gen + C::NST * C::STAGE + C::MERGE;
+    const uint32_t bars = base + C::NST * C::STAGE + C::MERGE;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (C::NST + s); };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 16 * C::NST);
+    RangeStart* start = reinterpret_cast<RangeStart*>(tail + 16 * C::NST + 16);
+    float* ml = reinterpret_cast<float*>(tail + C::TAIL_ML);                             // [NW][16][2]
+    static_assert(16 + sizeof(RangeStart) <= 64, "flag and range fit before the maxima");
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::NST; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), C::NW);
+        }
+        *abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tensormap(&k_map);
+        prefetch_tensormap(&v_map);
+    }
+    find_range<C::THREADS>(a, C::BK, 16, blockIdx.x, gridDim.x, start);
+    __syncthreads();
+    long long left = start->count;
+    int r = start->list;
+    long long off = start->offset;
+    const bool report = blockIdx.x == 0;
+    long long block_no = 0;
+    bool ok = true;
+
+    if (warp == C::NW) {
+        // ------------------------------------------------------------------------------ producer
+        const int box_shift = a.shift < 6 ? a.shift : 6;                 // rows per box: a page, at most 64
+        const int box_rows = 1 << box_shift;
+        const int subs = C::BK >> box_shift;
+        while (left > 0) {
+            const ListInfo li = list_info(a, r, report && lane == 0);
+            const long long nb = blocks_of(li.n, C::BK), units = nb * tiles_of(li, a, 16);
+            if (units == 0) {
+                ++r;
+                off = 0;
+                continue;
+            }
+            const int b0 = (int)(off % nb), cnt = (int)(left < nb - b0 ? left : nb - b0);
+            const int entries = (int)(((unsigned)li.n + (1u << a.shift) - 1u) >> a.shift);
+            const int32_t* tab = a.table + (size_t)r * a.max_pages;
+            // table entries ride in registers, 32 ahead of the 32 in use
+            auto entry = [&](int e) {
+                int page = 0;
+                if (e < entries) {
+                    page = tab[e];
+                    if ((unsigned)page >= (unsigned)a.n_pages) {
+                        a.status[1] = (int)EA_ERR_PAGES;
+                        page = 0;
+                    }
+                }
+                return page;
+            };
+            int win = ((b0 * C::BK) >> a.shift) & ~31;
+            int cur = entry(win + lane), next = entry(win + 32 + lane);
+            for (int b = b0; b < b0 + cnt; ++b, ++block_no) {
+                const int s = (int)(block_no % C::NST);
+                const uint32_t use = (uint32_t)(block_no / C::NST);
+                const int e0 = (b * C::BK) >> a.shift;
+                if (e0 >= win + 32) {
+                    win += 32;
+                    cur = next;
+                    next = entry(win + 32 + lane);
+                }
+                if (ok) ok = mbar_wait(empty(s), (use & 1) ^ 1, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) continue;
+                const int rest = li.n - b * C::BK;
+                int act = rest <= 0 ? 0 : (rest + box_rows - 1) >> box_shift;
+                if (act > subs) act = subs;
+                if (lane == 0) mbar_arrive_expect_tx(full(s), (uint32_t)(act * C::CHUNKS * 2 * box_rows * 128));
+                __syncwarp();
+                const uint32_t dst = base + (uint32_t)(s * C::STAGE);
+                const int boxes = act * C::CHUNKS * 2;
+                for (int i0 = 0; i0 < boxes; i0 += 32) {
+                    const int i = i0 + lane;
+                    const int sub = i / (C::CHUNKS * 2), c = i % C::CHUNKS, kv = (i / C::CHUNKS) & 1;
+                    const int key = b * C::BK + (sub << box_shift);
+                    const int page = __shfl_sync(0xffffffffu, cur, ((key >> a.shift) - win) & 31);
+                    if (i < boxes) {
+                        const uint32_t to = dst + (uint32_t)((kv * C::CHUNKS + c) * C::CHUNK_BYTES + (sub << box_shift) * 128);
+                        tma_load_3d(to, kv ? &v_map : &k_map, full(s), c * 64, key & ((1 << a.shift) - 1), page);
+                    }
+                }
+            }
+            left -= cnt;
+            off += cnt;
+            if (off == units) {
+                ++r;
+                off = 0;
+            }
+        }
+        if (!ok && lane == 0) {
+            // copies in flight land before the shared memory goes away
+            for (int s = 0; s < C::NST; ++s) {
+                mbar_drain(full(s), 0);
+                mbar_drain(full(s), 1);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------------------ consumers
+        const int g8 = lane >> 2, t4 = lane & 3;
+        // ldmatrix row addresses inside a stage (K: keys by channels; V: transposed on the way)
+        const int lm = lane >> 3, lr = lane & 7;
+        const uint32_t k_row = (uint32_t)(warp * 16 + (lm >> 1) * 8 + lr) * 128u;
+        const uint32_t v_row = (uint32_t)(warp * 16 + (lm & 1) * 8 + lr) * 128u;
+        const uint32_t sw = (uint32_t)lr << 4;
+        while (left > 0) {
+            const ListInfo li = list_info(a, r, false);
+            const long long nb = blocks_of(li.n, C::BK), units = nb * tiles_of(li, a, 16);
+            if (units == 0) {
+                ++r;
+                off = 0;
+                continue;
+            }
+            const int tile = (int)(off / nb), b0 = (int)(off % nb), cnt = (int)(left < nb - b0 ? left : nb - b0);
+            const int head0 = (r % a.Hkv) * a.G;
+            // rows g8 and g8 + 8 of the tile
+            int tok[2], hd[2], lim[2];
+            bool live[2];
+            uint32_t qf[D / 16][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int pr = tile * 16 + g8 + 8 * x;
+                tok[x] = pr / a.G;
+                hd[x] = head0 + pr % a.G;
+                live[x] = tok[x] < li.rows_tok;
+                const long long v = a.causal ? (long long)li.n - li.m + tok[x] + 1 : li.n;
+                lim[x] = !live[x] || v < 0 ? 0 : (int)(v < li.n ? v : li.n);
+                const __nv_bfloat16* src = a.q + (long long)(li.q0 + (live[x] ? tok[x] : 0)) * a.q_stride + (long long)hd[x] * D;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    qf[ks][x] = live[x] ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + t4 * 2) : 0u;
+                    qf[ks][x + 2] = live[x] ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + t4 * 2) : 0u;
+                }
+            }
+            float o[D / 8][4];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+
+            for (int b = b0; b < b0 + cnt; ++b, ++block_no) {
+                const int s = (int)(block_no % C::NST);
+                const uint32_t use = (uint32_t)(block_no / C::NST);
+                if (ok) ok = mbar_wait(full(s), use & 1, abort_flag);
+                const int key0 = b * C::BK + warp * 16;
+                if (key0 < li.n) {
+                    const uint32_t ks_base = base + (uint32_t)(s * C::STAGE);
+                    float x0[4] = {0.f, 0.f, 0.f, 0.f}, x1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        uint32_t kf[4];
+                        const uint32_t col = (uint32_t)((ks % 4) * 32 + (lm & 1) * 16);
+                        ldmatrix_x4(ks_base + (ks / 4) * C::CHUNK_BYTES + k_row + (col ^ sw), kf);
+                        mma_bf16(x0, qf[ks], kf[0], kf[1]);
+                        mma_bf16(x1, qf[ks], kf[2], kf[3]);
+                    }
+                    const int ka = key0 + t4 * 2;
+                    float y[2][4];
+                    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        y[x][0] = ka < lim[x] ? x0[2 * x] * a.scale_log2 : -INFINITY;
+                        y[x][1] = ka + 1 < lim[x] ? x0[2 * x + 1] * a.scale_log2 : -INFINITY;
+                        y[x][2] = ka + 8 < lim[x] ? x1[2 * x] * a.scale_log2 : -INFINITY;
+                        y[x][3] = ka + 9 < lim[x] ? x1[2 * x + 1] * a.scale_log2 : -INFINITY;
+                        top[x] = fmaxf(fmaxf(y[x][0], y[x][1]), fmaxf(y[x][2], y[x][3]));
+                        top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 1));
+                        top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 2));
+                    }
+                    if (__any_sync(0xffffffffu, top[0] > mx[0] || top[1] > mx[1])) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float m_new = fmaxf(mx[x], top[x]);
+                            const float f = m_new == -INFINITY ? 1.f : ex2(mx[x] - m_new);
+                            mx[x] = m_new;
+                            sum[x] *= f;
+#pragma unroll
+                            for (int i = 0; i < D / 8; ++i) {
+                                o[i][2 * x] *= f;
+                                o[i][2 * x + 1] *= f;
+                            }
+                        }
+                    }
+                    uint32_t pf[4];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float z = mx[x] == -INFINITY ? 0.f : mx[x];          // a row that has seen no key yet
+                        const float p0 = ex2(y[x][0] - z), p1 = ex2(y[x][1] - z), p2 = ex2(y[x][2] - z), p3 = ex2(y[x][3] - z);
+                        sum[x] += (p0 + p1) + (p2 + p3);
+                        pf[x] = pack_bf16(p0, p1);           // the weights enter the product with 8 significant bits
+                        pf[x + 2] = pack_bf16(p2, p3);
+                    }
+                    const uint32_t vs_base = ks_base + C::CHUNKS * C::CHUNK_BYTES;
+                    // rows behind the list's end hold anything: a weight of zero does not silence a NaN
+                    uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+                    if (key0 + 16 > li.n) {
+                        keep0 = (ka < li.n ? 0xffffu : 0u) | (ka + 1 < li.n ? 0xffff0000u : 0u);
+                        keep1 = (ka + 8 < li.n ? 0xffffu : 0u) | (ka + 9 < li.n ? 0xffff0000u : 0u);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < D / 16; ++nt) {
+                        uint32_t vf[4];
+                        const uint32_t col = (uint32_t)((nt % 4) * 32 + (lm >> 1) * 16);
+                        ldmatrix_x4_trans(vs_base + (nt / 4) * C::CHUNK_BYTES + v_row + (col ^ sw), vf);
+                        mma_bf16(o[2 * nt], pf, vf[0] & keep0, vf[1] & keep1);
+                        mma_bf16(o[2 * nt + 1], pf, vf[2] & keep0, vf[3] & keep1);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty(s));
+            }
+
+            // the warps' shares of the list: one maximum, then a tree of additions in a fixed order
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                sum[x] += __shfl_xor_sync(0xffffffffu, sum[x], 1);
+                sum[x] += __shfl_xor_sync(0xffffffffu, sum[x], 2);
+                if (t4 == 0) {
+                    ml[(warp * 16 + g8 + 8 * x) * 2] = mx[x];
+                    ml[(warp * 16 + g8 + 8 * x) * 2 + 1] = sum[x];
+                }
+            }
+            bar_sync(1, C::NW * 32);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float m_all = -INFINITY, l_all = 0.f;
+#pragma unroll
+                for (int w = 0; w < C::NW; ++w) m_all = fmaxf(m_all, ml[(w * 16 + g8 + 8 * x) * 2]);
+                const float z = m_all == -INFINITY ? 0.f : m_all;
+#pragma unroll
+                for (int w = 0; w < C::NW; ++w) l_all += ml[(w * 16 + g8 + 8 * x) * 2 + 1] * ex2(ml[(w * 16 + g8 + 8 * x) * 2] - z);
+                const float f = ex2(mx[x] - z);
+                mx[x] = m_all;
+                sum[x] = l_all;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    o[i][2 * x] *= f;
+                    o[i][2 * x + 1] *= f;
+                }
+            }
+#pragma unroll
+            for (int h = C::NW / 2; h >= 1; h /= 2) {
+                if (warp >= h && warp < 2 * h) {
+                    float4* dst = reinterpret_cast<float4*>(merge) + (size_t)(h == C::NW / 2 ? warp - h : warp) * (D / 8) * 32 + lane;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) dst[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+                }
+                bar_sync(1, C::NW * 32);
+                if (warp < h) {
+                    const float4* src = reinterpret_cast<const float4*>(merge) + (size_t)(h == C::NW / 2 ? warp : warp + h) * (D / 8) * 32 + lane;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const float4 v = src[i * 32];
+                        o[i][0] += v.x;
+                        o[i][1] += v.y;
+                        o[i][2] += v.z;
+                        o[i][3] += v.w;
+                    }
+                }
+            }
+            if (warp == 0) {
+                const bool whole = b0 == 0 && cnt == nb;
+                const size_t slot = 2 * (size_t)blockIdx.x + (start->count == left ? 0 : 1);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!live[x]) continue;
+                    if (whole) {
+                        const float inv = sum[x] > 0.f ? 1.f / sum[x] : (sum[x] == 0.f ? 0.f : sum[x]);
+                        const size_t row = (size_t)(li.q0 + tok[x]) * a.Hq + hd[x];
+                        uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D) + t4;
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) dst[i * 4] = pack_bf16(o[i][2 * x] * inv, o[i][2 * x + 1] * inv);
+                        if (a.lse && t4 == 0) a.lse[row] = lse_of(mx[x], sum[x]);
+                    } else {
+                        const size_t row = slot * 16 + g8 + 8 * x;
+                        float2* dst = reinterpret_cast<float2*>(a.part_o + row * D) + t4;
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) dst[i * 4] = make_float2(o[i][2 * x], o[i][2 * x + 1]);
+                        if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + row * 2) = make_float2(mx[x], sum[x]);
+                    }
+                }
+            }
+            left -= cnt;
+            off += cnt;
+            if (off == units) {
+                ++r;
+                off = 0;
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
+}
+
+// Joins the partial results of row tiles (ROWS rows) that several CTAs shared: one CTA per (tile, list).
+template <int D, int ROWS>
+__global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, int BK, int ctas) {
+    const int r = blockIdx.y, tile = blockIdx.x;
+    const ListInfo li = list_info(a, r, false);
+    if (tile >= tiles_of(li, a, ROWS)) return;
+    // units before this list, and in all
+    long long before, total;
+    count_units<128>(a, BK, ROWS, r, &before, &total);
+    const long long nb = blocks_of(li.n, BK);
+    const long long u0 = before + tile * nb, u1 = u0 + nb;
+    const int c0 = owner_of(u0, total, ctas), c1 = owner_of(u1 - 1, total, ctas);
+    if (c0 == c1) return;
+    const int slot0 = u0 > range_begin(c0, total, ctas) ? 2 * c0 + 1 : 2 * c0;
+    for (int i = threadIdx.x; i < ROWS * (D / 4); i += 128) {
+        const int row = i / (D / 4), col = i % (D / 4);
+        const int pr = tile * ROWS + row, tok = pr / a.G;
+        if (tok >= li.rows_tok) break;
+        float m = -INFINITY;
+        for (int c = c0; c <= c1; ++c)
+            if (owns_some(c, total, ctas)) m = fmaxf(m, a.part_ml[((size_t)(c == c0 ? slot0 : 2 * c) * ROWS + row) * 2]);
+        const float z = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = c0; c <= c1; ++c) {
+            if (!owns_some(c, total, ctas)) continue;
+            const size_t at = (size_t)(c == c0 ? slot0 : 2 * c) * ROWS + row;
+            const float2 p = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+            const float f = ex2(p.x - z);
+            const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * D + col * 4);
+            l += p.y * f;
+            o.x += v.x * f;
+            o.y += v.y * f;
+            o.z += v.z * f;
+            o.w += v.w * f;
+        }
+        const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+        const size_t at = (size_t)(li.q0 + tok) * a.Hq + (r % a.Hkv) * a.G + pr % a.G;
+        *reinterpret_cast<uint2*>(a.out + at * D + col * 4) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (a.lse && col == 0) a.lse[at] = lse_of(m, l);
+    }
+}
+
+constexpr int kMaxCtas = 256;                 // grid of the persistent kernels, at most
+
+size_t few_part_floats(int d) { return (size_t)2 * kMaxCtas * 16 * (d + 2); }
+
+template <int D>
+ea_status launch_few(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& args, const void* k_pages, const void* v_pages,
+                     cudaStream_t st) {
+    using C = Few<D>;
+    AttnArgs a = args;
+    const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
+    a.part_o = static_cast<float*>(ctx->workspace);
+    a.part_ml = a.part_o + (size_t)2 * kMaxCtas * 16 * D;
+    CUtensorMap k_map, v_map;
+    const uint32_t box = s.page_rows < 64 ? (uint32_t)s.page_rows : 64u;
+    const uint64_t row = (uint64_t)D * 2, page = row * s.page_rows;
+    // an empty pool is never read (list_info refuses every row of it), but a map needs an address and a size
+    const uint64_t pages = s.n_pages > 0 ? (uint64_t)s.n_pages : 1;
+    const void *kp = s.n_pages > 0 ? k_pages : ctx->workspace, *vp = s.n_pages > 0 ? v_pages : ctx->workspace;
+    if (!ea_tensor_map_bf16_3d(&k_map, kp, D, (uint64_t)s.page_rows, pages, row, page, 64, box) ||
+        !ea_tensor_map_bf16_3d(&v_map, vp, D, (uint64_t)s.page_rows, pages, row, page, 64, box))
+        return EA_ERR_CUDA;
+    auto kernel = paged_few_kernel<D>;
+    EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
+    const long long tiles = ((long long)a.max_q * a.G + 15) / 16;
+    paged_combine_kernel<D, 16><<<dim3((unsigned)tiles, (unsigned)(s.n_seqs * s.n_kv_heads)), 128, 0, st>>>(a, C::BK, ctas);
+    ea_count_launches(ctx, 2);
+    return EA_CHECK_LAUNCH();
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace
+
+size_t ea_paged_attn_ws_bytes(const ea_paged_shape& s, int max_q) {
+    (void)max_q;
+    return few_part_floats(s.head_dim) * sizeof(float);
+}
+
+extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape, const void* q, int64_t q_stride, int32_t n_tokens,
+                                        const int32_t* q_offsets, int32_t max_q, const int32_t* kv_lens, const int32_t* block_table,
+                                        const void* k_pages, const void* v_pages, float scale, int32_t causal, void* out,
+                                        float* lse_opt, void* cuda_stream) {
+    if (!ctx) return EA_ERR_INVALID_ARG;
+    ea_status st = ea_check_paged_shape(shape);
+    if (st != EA_OK) return st;
+    if (n_tokens < 0 || max_q < 0 || max_q > n_tokens || !(fabsf(scale) <= 3.0e38f)) return EA_ERR_INVALID_ARG;
+    const int64_t dense = (int64_t)shape->n_q_heads * shape->head_dim;
+    if (q_stride == 0) q_stride = dense;
+    if (q_stride < dense || q_stride % 8 != 0) return EA_ERR_INVALID_ARG;
+    if ((int64_t)n_tokens * shape->n_q_heads > 0x7fffffffLL) return EA_ERR_UNSUPPORTED;
+    if (shape->n_seqs == 0 || n_tokens == 0 || max_q == 0) return EA_OK;
+    if (!q || !q_offsets || !kv_lens || !out || (shape->max_pages > 0 && !block_table)) return EA_ERR_INVALID_ARG;
+    if (shape->n_pages > 0 && (!k_pages || !v_pages)) return EA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned4(q_offsets) || !aligned4(kv_lens) ||
+        !aligned4(block_table) || !aligned4(lse_opt))
+        return EA_ERR_INVALID_ARG;
+    if (ctx->workspace_bytes < ea_paged_attn_ws_bytes(*shape, max_q)) return EA_ERR_WORKSPACE;
+    AttnArgs a = {};
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.q_stride = q_stride;
+    a.q_off = q_offsets;
+    a.kv_len = kv_lens;
+    a.table = block_table;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.lse = lse_opt;
+    a.status = ctx->status_dev;
+    a.lists = shape->n_seqs * shape->n_kv_heads;
+    a.Hq = shape->n_q_heads;
+    a.Hkv = shape->n_kv_heads;
+    a.G = shape->n_q_heads / shape->n_kv_heads;
+    a.shift = __builtin_ctz((unsigned)shape->page_rows);
+    a.n_pages = shape->n_pages;
+    a.max_pages = shape->max_pages;
+    a.n_tokens = n_tokens;
+    a.max_q = max_q;
+    a.causal = causal != 0;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    int prev = 0;
+    EA_CUDA_TRY(cudaGetDevice(&prev));
+    if (prev != ctx->device) EA_CUDA_TRY(cudaSetDevice(ctx->device));
+    ctx->image_ready = false;                       // the partial results lie where fused statistics keep their images
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    st = shape->head_dim == 64    ? launch_few<64>(ctx, *shape, a, k_pages, v_pages, stream)
+         : shape->head_dim == 128 ? launch_few<128>(ctx, *shape, a, k_pages, v_pages, stream)
+                                  : launch_few<256>(ctx, *shape, a, k_pages, v_pages, stream);
+    if (prev != ctx->device) cudaSetDevice(prev);
+    return st;
+}

@@ -1,0 +1,186 @@
+// What the attention kernels over the paged cache share: the description of a list, the division of the call's key
+// blocks among the CTAs, and small wrappers.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "ea_internal.h"
+
+struct AttnArgs {
+    const __nv_bfloat16* q;
+    long long q_stride;          // elements between tokens
+    const int32_t* q_off;        // [n_seqs + 1]
+    const int32_t* kv_len;       // [lists]
+    const int32_t* table;        // [lists][max_pages]
+    __nv_bfloat16* out;          // [n_tokens, Hq, d]
+    float* lse;                  // [n_tokens, Hq] or nullptr
+    float* part_o;               // unnormalised partial outputs, two row tiles per CTA
+    float* part_ml;              // their maxima (of scores in units of log 2) and sums
+    int* status;
+    int lists, Hq, Hkv, G, shift, n_pages, max_pages, n_tokens, max_q, causal;
+    float scale_log2;
+};
+
+struct ListInfo {
+    int m;                       // new tokens of the sequence
+    int rows_tok;                // of them, those that the call serves (max_q at most)
+    int q0;                      // the first one's row in q
+    int n;                       // rows of the list
+};
+
+// Lengths and offsets live on the device, so they are checked here: what does not fit is reported and left out.
+__device__ __forceinline__ ListInfo list_info(const AttnArgs& a, int r, bool report) {
+    const int s = r / a.Hkv;
+    const int q0 = a.q_off[s], q1 = a.q_off[s + 1];
+    ListInfo li = {0, 0, 0, 0};
+    bool bad = q0 < 0 || q1 < q0 || q1 > a.n_tokens;
+    if (!bad) {
+        li.m = q1 - q0;
+        li.q0 = q0;
+        li.rows_tok = li.m < a.max_q ? li.m : a.max_q;
+        bad = li.m > a.max_q;
+    }
+    const long long cap = a.n_pages > 0 ? (long long)a.max_pages << a.shift : 0;
+    int n = a.kv_len[r];
+    if (n < 0 || n > cap) {
+        bad = true;
+        n = n < 0 ? 0 : (int)cap;
+    }
+    li.n = n;
+    if (bad && report) a.status[1] = (int)EA_ERR_PAGES;
+    return li;
+}
+// Key blocks of a list: one at least, so that a list without rows still has its outputs written.
+__device__ __forceinline__ long long blocks_of(int n, int BK) { return n > BK ? ((long long)n + BK - 1) / BK : 1; }
+__device__ __forceinline__ int tiles_of(const ListInfo& li, const AttnArgs& a, int rows) {
+    return (int)(((long long)li.rows_tok * a.G + rows - 1) / rows);
+}
+
+// CTA c of n takes units [c W / n, (c + 1) W / n) of the call's W units (unit: one key block of one row tile).
+__device__ __forceinline__ long long range_begin(int c, long long total, int ctas) { return (long long)c * total / ctas; }
+__device__ __forceinline__ int owner_of(long long unit, long long total, int ctas) {
+    return (int)(((unit + 1) * ctas - 1) / total);
+}
+// (fewer units than CTAs: some own none, and leave nothing behind)
+__device__ __forceinline__ bool owns_some(int c, long long total, int ctas) {
+    return range_begin(c, total, ctas) < range_begin(c + 1, total, ctas);
+}
+
+struct RangeStart {
+    long long first, count, offset;      // first unit and number of units; offset of the first inside its list
+    int list;
+};
+
+__device__ __forceinline__ long long scan_up_ll(long long v, int d) { return __shfl_up_sync(0xffffffffu, v, d); }
+
+// Where the CTA's share of the units begins.  Every thread calls it; *out (shared memory) is valid after the
+// caller's next __syncthreads.  Reports lists that do not fit (CTA 0).
+template <int THREADS>
+__device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int ctas, RangeStart* out) {
+    __shared__ long long warp_sum[THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.lists + THREADS - 1) / THREADS;
+    const int r0 = min(a.lists, tid * per), r1 = min(a.lists, r0 + per);
+    long long mine = 0;
+    for (int r = r0; r < r1; ++r) {
+        const ListInfo li = list_info(a, r, cta == 0);
+        mine += blocks_of(li.n, BK) * tiles_of(li, a, rows);
+    }
+    long long inc = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long x = scan_up_ll(inc, d);
+        if (lane >= d) inc += x;
+    }
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    long long before = 0, total = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w == warp) before = total;
+        total += warp_sum[w];
+    }
+    long long at = before + inc - mine;
+    const long long first = total > 0 ? range_begin(cta, total, ctas) : 0;
+    const long long end = total > 0 ? range_begin(cta + 1, total, ctas) : 0;
+    if (tid == 0) {
+        out->first = first;
+        out->count = end - first;
+        out->list = 0;
+        out->offset = 0;
+    }
+    __syncthreads();
+    if (end > first && first >= at && first < at + mine) {
+        for (int r = r0; r < r1; ++r) {
+            const ListInfo li = list_info(a, r, false);
+            const long long units = blocks_of(li.n, BK) * tiles_of(li, a, rows);
+            if (first < at + units) {
+                out->list = r;
+                out->offset = first - at;
+                break;
+            }
+            at += units;
+        }
+    }
+}
+
+// Units of the lists before `list`, and of all.  Every thread calls it and gets both.
+template <int THREADS>
+__device__ void count_units(const AttnArgs& a, int BK, int rows, int list, long long* before, long long* total) {
+    __shared__ long long warp_before[THREADS / 32], warp_total[THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    long long b = 0, t = 0;
+    for (int r = tid; r < a.lists; r += THREADS) {
+        const ListInfo li = list_info(a, r, false);
+        const long long units = blocks_of(li.n, BK) * tiles_of(li, a, rows);
+        t += units;
+        if (r < list) b += units;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        b += __shfl_xor_sync(0xffffffffu, b, d);
+        t += __shfl_xor_sync(0xffffffffu, t, d);
+    }
+    if (lane == 0) {
+        warp_before[warp] = b;
+        warp_total[warp] = t;
+    }
+    __syncthreads();
+    b = t = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+        b += warp_before[w];
+        t += warp_total[w];
+    }
+    *before = b;
+    *total = t;
+}
+
+// ---- wrappers
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// m: maximum of the scores in units of log 2, l: sum of 2^(score - m)
+__device__ __forceinline__ float lse_of(float m, float l) {
+    return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&x)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
+}
