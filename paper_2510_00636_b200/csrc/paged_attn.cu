@@ -51,9 +51,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (C::NST + s); };
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 16 * C::NST);
-    RangeStart* start = reinterpret_cast<RangeStart*>(tail + 16 * C::NST + 16);
+    Walk* start = reinterpret_cast<Walk*>(tail + 16 * C::NST + 16);
     float* ml = reinterpret_cast<float*>(tail + C::TAIL_ML);                             // [NW][16][2]
-    static_assert(16 + sizeof(RangeStart) <= 64, "flag and range fit before the maxima");
+    static_assert(16 + sizeof(Walk) <= 64, "flag and range fit before the maxima");
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
@@ -68,10 +68,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     }
     find_range<C::THREADS>(a, C::BK, 16, blockIdx.x, gridDim.x, start);
     __syncthreads();
-    long long left = start->count;
-    int r = start->list;
-    long long off = start->offset;
-    const bool report = blockIdx.x == 0;
+    Walk walk = *start;
+    Item it;
     long long block_no = 0;
     bool ok = true;
 
@@ -80,15 +78,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         const int box_shift = a.shift < 6 ? a.shift : 6;                 // rows per box: a page, at most 64
         const int box_rows = 1 << box_shift;
         const int subs = C::BK >> box_shift;
-        while (left > 0) {
-            const ListInfo li = list_info(a, r, report && lane == 0);
-            const long long nb = blocks_of(li.n, C::BK), units = nb * tiles_of(li, a, 16);
-            if (units == 0) {
-                ++r;
-                off = 0;
-                continue;
-            }
-            const int b0 = (int)(off % nb), cnt = (int)(left < nb - b0 ? left : nb - b0);
+        while (next_item(a, walk, 16, C::BK, it)) {
+            const ListInfo& li = it.li;
+            const int r = it.list, b0 = it.b0;
             const int entries = (int)(((unsigned)li.n + (1u << a.shift) - 1u) >> a.shift);
             const int32_t* tab = a.table + (size_t)r * a.max_pages;
             // table entries ride in registers, 32 ahead of the 32 in use
@@ -105,7 +97,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             };
             int win = ((b0 * C::BK) >> a.shift) & ~31;
             int cur = entry(win + lane), next = entry(win + 32 + lane);
-            for (int b = b0; b < b0 + cnt; ++b, ++block_no) {
+            for (int b = b0; b < it.b1; ++b, ++block_no) {
                 const int s = (int)(block_no % C::NST);
                 const uint32_t use = (uint32_t)(block_no / C::NST);
                 const int e0 = (b * C::BK) >> a.shift;
@@ -135,12 +127,6 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     }
                 }
             }
-            left -= cnt;
-            off += cnt;
-            if (off == units) {
-                ++r;
-                off = 0;
-            }
         }
         if (!ok && lane == 0) {
             // copies in flight land before the shared memory goes away
@@ -158,16 +144,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         const uint32_t k_row = (uint32_t)(warp * 16 + (lm >> 1) * 8 + lr) * 128u;
         const uint32_t v_row = (uint32_t)(warp * 16 + (lm & 1) * 8 + lr) * 128u;
         const uint32_t sw = (uint32_t)lr << 4;
-        while (left > 0) {
-            const ListInfo li = list_info(a, r, false);
-            const long long nb = blocks_of(li.n, C::BK), units = nb * tiles_of(li, a, 16);
-            if (units == 0) {
-                ++r;
-                off = 0;
-                continue;
-            }
-            const int tile = (int)(off / nb), b0 = (int)(off % nb), cnt = (int)(left < nb - b0 ? left : nb - b0);
-            const int head0 = (r % a.Hkv) * a.G;
+        while (next_item(a, walk, 16, C::BK, it)) {
+            const ListInfo& li = it.li;
+            const int tile = it.tile, b0 = it.b0;
+            const int head0 = (it.list % a.Hkv) * a.G;
             // rows g8 and g8 + 8 of the tile
             int tok[2], hd[2], lim[2];
             bool live[2];
@@ -178,8 +158,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 tok[x] = pr / a.G;
                 hd[x] = head0 + pr % a.G;
                 live[x] = tok[x] < li.rows_tok;
-                const long long v = a.causal ? (long long)li.n - li.m + tok[x] + 1 : li.n;
-                lim[x] = !live[x] || v < 0 ? 0 : (int)(v < li.n ? v : li.n);
+                lim[x] = live[x] ? limit_of(li, a, tok[x]) : 0;
                 const __nv_bfloat16* src = a.q + (long long)(li.q0 + (live[x] ? tok[x] : 0)) * a.q_stride + (long long)hd[x] * D;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
@@ -192,7 +171,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
             float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 
-            for (int b = b0; b < b0 + cnt; ++b, ++block_no) {
+            for (int b = b0; b < it.b1; ++b, ++block_no) {
                 const int s = (int)(block_no % C::NST);
                 const uint32_t use = (uint32_t)(block_no / C::NST);
                 if (ok) ok = mbar_wait(full(s), use & 1, abort_flag);
@@ -313,8 +292,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 }
             }
             if (warp == 0) {
-                const bool whole = b0 == 0 && cnt == nb;
-                const size_t slot = 2 * (size_t)blockIdx.x + (start->count == left ? 0 : 1);
+                const bool whole = b0 == 0 && it.b1 == it.blocks;
+                const size_t slot = 2 * (size_t)blockIdx.x + (it.first ? 0 : 1);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (!live[x]) continue;
@@ -334,12 +313,6 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     }
                 }
             }
-            left -= cnt;
-            off += cnt;
-            if (off == units) {
-                ++r;
-                off = 0;
-            }
         }
     }
     __syncthreads();
@@ -355,8 +328,9 @@ __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, in
     // units before this list, and in all
     long long before, total;
     count_units<128>(a, BK, ROWS, r, &before, &total);
-    const long long nb = blocks_of(li.n, BK);
-    const long long u0 = before + tile * nb, u1 = u0 + nb;
+    long long u0 = before;
+    for (int t = 0; t < tile; ++t) u0 += tile_blocks(li, a, t, ROWS, BK);
+    const long long u1 = u0 + tile_blocks(li, a, tile, ROWS, BK);
     const int c0 = owner_of(u0, total, ctas), c1 = owner_of(u1 - 1, total, ctas);
     if (c0 == c1) return;
     const int slot0 = u0 > range_begin(c0, total, ctas) ? 2 * c0 + 1 : 2 * c0;
@@ -389,34 +363,26 @@ __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, in
     }
 }
 
-constexpr int kMaxCtas = 256;                 // grid of the persistent kernels, at most
-
-size_t few_part_floats(int d) { return (size_t)2 * kMaxCtas * 16 * (d + 2); }
+size_t few_part_floats(int d) { return (size_t)2 * kPagedMaxCtas * 16 * (d + 2); }
 
 template <int D>
 ea_status launch_few(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& args, const void* k_pages, const void* v_pages,
                      cudaStream_t st) {
     using C = Few<D>;
     AttnArgs a = args;
-    const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
+    const int ctas = ctx->sm_count < kPagedMaxCtas ? ctx->sm_count : kPagedMaxCtas;
     a.part_o = static_cast<float*>(ctx->workspace);
-    a.part_ml = a.part_o + (size_t)2 * kMaxCtas * 16 * D;
+    a.part_ml = a.part_o + (size_t)2 * kPagedMaxCtas * 16 * D;
     CUtensorMap k_map, v_map;
     const uint32_t box = s.page_rows < 64 ? (uint32_t)s.page_rows : 64u;
-    const uint64_t row = (uint64_t)D * 2, page = row * s.page_rows;
-    // an empty pool is never read (list_info refuses every row of it), but a map needs an address and a size
-    const uint64_t pages = s.n_pages > 0 ? (uint64_t)s.n_pages : 1;
-    const void *kp = s.n_pages > 0 ? k_pages : ctx->workspace, *vp = s.n_pages > 0 ? v_pages : ctx->workspace;
-    if (!ea_tensor_map_bf16_3d(&k_map, kp, D, (uint64_t)s.page_rows, pages, row, page, 64, box) ||
-        !ea_tensor_map_bf16_3d(&v_map, vp, D, (uint64_t)s.page_rows, pages, row, page, 64, box))
-        return EA_ERR_CUDA;
+    if (!ea_paged_map(ctx, s, k_pages, box, &k_map) || !ea_paged_map(ctx, s, v_pages, box, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_few_kernel<D>;
     EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
     kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
-    const long long tiles = ((long long)a.max_q * a.G + 15) / 16;
-    paged_combine_kernel<D, 16><<<dim3((unsigned)tiles, (unsigned)(s.n_seqs * s.n_kv_heads)), 128, 0, st>>>(a, C::BK, ctas);
-    ea_count_launches(ctx, 2);
-    return EA_CHECK_LAUNCH();
+    ea_count_launches(ctx, 1);
+    ea_status err = EA_CHECK_LAUNCH();
+    if (err != EA_OK) return err;
+    return ea_launch_paged_combine(ctx, s, a, 16, C::BK, ctas, st);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -424,9 +390,31 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 }  // namespace
 
+bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t box_rows, CUtensorMap* map) {
+    const uint64_t row = (uint64_t)s.head_dim * 2, page = row * s.page_rows;
+    // an empty pool is never read (list_info refuses every row of it), but a map needs an address and a size
+    const uint64_t n = s.n_pages > 0 ? (uint64_t)s.n_pages : 1;
+    return ea_tensor_map_bf16_3d(map, s.n_pages > 0 ? pages : ctx->workspace, (uint64_t)s.head_dim, (uint64_t)s.page_rows, n, row, page, 64,
+                                 box_rows);
+}
+
+ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st) {
+    const dim3 grid((unsigned)(((long long)a.max_q * a.G + rows - 1) / rows), (unsigned)(s.n_seqs * s.n_kv_heads));
+    const int d = s.head_dim;
+    auto kernel = rows == 16    ? (d == 64 ? paged_combine_kernel<64, 16> : d == 128 ? paged_combine_kernel<128, 16> : paged_combine_kernel<256, 16>)
+                  : rows == 128 ? paged_combine_kernel<256, 128>
+                                : (d == 64 ? paged_combine_kernel<64, 256> : paged_combine_kernel<128, 256>);
+    kernel<<<grid, 128, 0, st>>>(a, BK, ctas);
+    ea_count_launches(ctx, 1);
+    return EA_CHECK_LAUNCH();
+}
+
+// Up to 16 rows per list fit one tile of the kernel for few rows; more go to the tensor-core tiles of 128.
+static bool few_rows(int max_q, int G) { return (long long)max_q * G <= 16; }
+
 size_t ea_paged_attn_ws_bytes(const ea_paged_shape& s, int max_q) {
-    (void)max_q;
-    return few_part_floats(s.head_dim) * sizeof(float);
+    const size_t few = few_part_floats(s.head_dim);
+    return (few_rows(max_q, s.n_q_heads / s.n_kv_heads) ? few : ea_paged_chunk_ws_floats(s.head_dim)) * sizeof(float);
 }
 
 extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape, const void* q, int64_t q_stride, int32_t n_tokens,
@@ -473,9 +461,12 @@ extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape
     if (prev != ctx->device) EA_CUDA_TRY(cudaSetDevice(ctx->device));
     ctx->image_ready = false;                       // the partial results lie where fused statistics keep their images
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    st = shape->head_dim == 64    ? launch_few<64>(ctx, *shape, a, k_pages, v_pages, stream)
-         : shape->head_dim == 128 ? launch_few<128>(ctx, *shape, a, k_pages, v_pages, stream)
-                                  : launch_few<256>(ctx, *shape, a, k_pages, v_pages, stream);
+    if (!few_rows(max_q, a.G))
+        st = ea_launch_paged_chunk(ctx, *shape, a, k_pages, v_pages, stream);
+    else
+        st = shape->head_dim == 64    ? launch_few<64>(ctx, *shape, a, k_pages, v_pages, stream)
+             : shape->head_dim == 128 ? launch_few<128>(ctx, *shape, a, k_pages, v_pages, stream)
+                                      : launch_few<256>(ctx, *shape, a, k_pages, v_pages, stream);
     if (prev != ctx->device) cudaSetDevice(prev);
     return st;
 }

@@ -50,10 +50,26 @@ __device__ __forceinline__ ListInfo list_info(const AttnArgs& a, int r, bool rep
     if (bad && report) a.status[1] = (int)EA_ERR_PAGES;
     return li;
 }
-// Key blocks of a list: one at least, so that a list without rows still has its outputs written.
-__device__ __forceinline__ long long blocks_of(int n, int BK) { return n > BK ? ((long long)n + BK - 1) / BK : 1; }
 __device__ __forceinline__ int tiles_of(const ListInfo& li, const AttnArgs& a, int rows) {
     return (int)(((long long)li.rows_tok * a.G + rows - 1) / rows);
+}
+// First row of a list that token `tok` does not see.
+__device__ __forceinline__ int limit_of(const ListInfo& li, const AttnArgs& a, int tok) {
+    if (!a.causal) return li.n;
+    const long long v = (long long)li.n - li.m + tok + 1;
+    return v < 0 ? 0 : v < li.n ? (int)v : li.n;
+}
+// Key blocks that a row tile looks at: one at least, so that rows which see nothing still have their outputs written.
+__device__ __forceinline__ int tile_blocks(const ListInfo& li, const AttnArgs& a, int tile, int rows, int BK) {
+    const long long last = (((long long)tile + 1) * rows - 1) / a.G;
+    const int lim = limit_of(li, a, last < li.rows_tok ? (int)last : li.rows_tok - 1);
+    return lim > BK ? (int)(((unsigned)lim + BK - 1u) / BK) : 1;
+}
+__device__ __forceinline__ long long list_units(const ListInfo& li, const AttnArgs& a, int rows, int BK) {
+    const int tiles = tiles_of(li, a, rows);
+    long long u = 0;
+    for (int t = 0; t < tiles; ++t) u += tile_blocks(li, a, t, rows, BK);
+    return u;
 }
 
 // CTA c of n takes units [c W / n, (c + 1) W / n) of the call's W units (unit: one key block of one row tile).
@@ -66,17 +82,46 @@ __device__ __forceinline__ bool owns_some(int c, long long total, int ctas) {
     return range_begin(c, total, ctas) < range_begin(c + 1, total, ctas);
 }
 
-struct RangeStart {
-    long long first, count, offset;      // first unit and number of units; offset of the first inside its list
-    int list;
+// A CTA's share: where it begins, and how many units it has.
+struct Walk {
+    long long count, left;
+    int list, tile, block;
 };
+// Consecutive units of one row tile.
+struct Item {
+    ListInfo li;
+    int list, tile, b0, b1, blocks;      // key blocks b0 .. b1 - 1 of `blocks`
+    bool first;                          // the CTA's first item
+};
+__device__ __forceinline__ bool next_item(const AttnArgs& a, Walk& w, int rows, int BK, Item& it) {
+    if (w.left <= 0) return false;
+    for (;;) {
+        it.li = list_info(a, w.list, false);
+        if (w.tile < tiles_of(it.li, a, rows)) break;
+        ++w.list;
+        w.tile = w.block = 0;
+    }
+    it.list = w.list;
+    it.tile = w.tile;
+    it.blocks = tile_blocks(it.li, a, w.tile, rows, BK);
+    it.b0 = w.block;
+    it.b1 = w.left < it.blocks - w.block ? w.block + (int)w.left : it.blocks;
+    it.first = w.left == w.count;
+    w.left -= it.b1 - it.b0;
+    w.block = it.b1;
+    if (w.block == it.blocks) {
+        ++w.tile;
+        w.block = 0;
+    }
+    return true;
+}
 
 __device__ __forceinline__ long long scan_up_ll(long long v, int d) { return __shfl_up_sync(0xffffffffu, v, d); }
 
 // Where the CTA's share of the units begins.  Every thread calls it; *out (shared memory) is valid after the
 // caller's next __syncthreads.  Reports lists that do not fit (CTA 0).
 template <int THREADS>
-__device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int ctas, RangeStart* out) {
+__device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int ctas, Walk* out) {
     __shared__ long long warp_sum[THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.lists + THREADS - 1) / THREADS;
@@ -84,7 +129,7 @@ __device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int cta
     long long mine = 0;
     for (int r = r0; r < r1; ++r) {
         const ListInfo li = list_info(a, r, cta == 0);
-        mine += blocks_of(li.n, BK) * tiles_of(li, a, rows);
+        mine += list_units(li, a, rows, BK);
     }
     long long inc = mine;
 #pragma unroll
@@ -103,22 +148,24 @@ __device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int cta
     const long long first = total > 0 ? range_begin(cta, total, ctas) : 0;
     const long long end = total > 0 ? range_begin(cta + 1, total, ctas) : 0;
     if (tid == 0) {
-        out->first = first;
-        out->count = end - first;
-        out->list = 0;
-        out->offset = 0;
+        out->count = out->left = end - first;
+        out->list = out->tile = out->block = 0;
     }
     __syncthreads();
     if (end > first && first >= at && first < at + mine) {
         for (int r = r0; r < r1; ++r) {
             const ListInfo li = list_info(a, r, false);
-            const long long units = blocks_of(li.n, BK) * tiles_of(li, a, rows);
-            if (first < at + units) {
-                out->list = r;
-                out->offset = first - at;
-                break;
+            const int tiles = tiles_of(li, a, rows);
+            for (int t = 0; t < tiles; ++t) {
+                const int nb = tile_blocks(li, a, t, rows, BK);
+                if (first < at + nb) {
+                    out->list = r;
+                    out->tile = t;
+                    out->block = (int)(first - at);
+                    return;
+                }
+                at += nb;
             }
-            at += units;
         }
     }
 }
@@ -131,7 +178,7 @@ __device__ void count_units(const AttnArgs& a, int BK, int rows, int list, long 
     long long b = 0, t = 0;
     for (int r = tid; r < a.lists; r += THREADS) {
         const ListInfo li = list_info(a, r, false);
-        const long long units = blocks_of(li.n, BK) * tiles_of(li, a, rows);
+        const long long units = list_units(li, a, rows, BK);
         t += units;
         if (r < list) b += units;
     }
@@ -153,6 +200,17 @@ __device__ void count_units(const AttnArgs& a, int BK, int rows, int list, long 
     *before = b;
     *total = t;
 }
+
+constexpr int kPagedMaxCtas = 160;             // grid of the persistent kernels, at most (one CTA per SM)
+
+// The pool as a rank-3 tensor (d, rows of a page, pages) in boxes of 64 channels x box_rows rows.
+bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t box_rows, CUtensorMap* map);
+// Joins what several CTAs left of a row tile.
+ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st);
+// Row tiles of 128 on the tensor cores (paged_chunk.cu).
+size_t ea_paged_chunk_ws_floats(int d);
+ea_status ea_launch_paged_chunk(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, const void* k_pages, const void* v_pages,
+                                cudaStream_t st);
 
 // ---- wrappers
 __device__ __forceinline__ float ex2(float x) {

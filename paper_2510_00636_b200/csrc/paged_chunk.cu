@@ -1,0 +1,482 @@
+// Attention of chunks of new tokens over the paged cache on the tensor cores (tcgen05).
+//
+// A CTA works on row tiles of 128 packed rows (row = token * G + head), two of them at head_dim <= 128, one at 256 (the
+// output of a tile takes head_dim of the 512 tensor-memory columns, its scores 128), against blocks of 128 keys:
+//     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
+//     P = 2^(c S - m)  one thread per row: running maximum m, sum l; P (bf16) over S in tensor memory
+//     O += P V         A = P from tensor memory, B = V as it lies (rows are the contraction index: MN-major)
+// One warp keeps K and V flowing through a ring of 16 KiB slots (TMA boxes of a page each), one thread issues the MMAs,
+// and four warps per row tile do the softmax.  With two row tiles the tensor cores work on one while the softmax works on
+// the other; with one, on the scores of the next block.
+//
+// The running maximum only moves when a row's scores exceed it by more than 2^8 (the weights then stay within fp32 and
+// bf16 range, and the sum, which uses the same maximum, cancels it): O is rescaled in tensor memory only then.
+//
+// The CTAs divide the call's (row tile, key block) units evenly, as in the kernel for few rows (paged_attn.cuh).
+#include "paged.h"
+#include "paged_attn.cuh"
+#include "ptx_sm100.cuh"
+
+using namespace ptx;
+
+namespace {
+
+constexpr int kBK = 128;                                // keys per block
+constexpr uint32_t kSlot = 16384;
+constexpr float kRescale = 8.0f;
+
+template <int D> struct Chunk {
+    static constexpr int TILES = D == 256 ? 1 : 2;
+    static constexpr int ROWS = TILES * 128;
+    static constexpr int KC = D / 64;                   // slots of a K block: 128 keys x 64 channels each
+    static constexpr int VKEYS = 8192 / D;              // keys of a V slot: all channels
+    static constexpr int VC = kBK / VKEYS;
+    static constexpr int PER_BLOCK = KC + VC;
+    static constexpr uint32_t Q_TILE = 128u * D * 2;
+    static constexpr int NSLOT = D == 64 ? 12 : 10;
+    static constexpr int THREADS = 64 + TILES * 128;
+    static constexpr int BARS = 2 * NSLOT + 9;
+    static constexpr int TAIL = BARS * 8 + 16 + (int)sizeof(Walk);
+    static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)kSlot + TAIL;
+    static constexpr uint32_t O_COL = 256;              // tensor memory: S (P) at 0 and 128, O from 256
+    static_assert(SMEM + 1024 <= 232448, "a CTA's shared memory, with room for static arrays");
+    // Order of the blocks in the ring, in slots after the item's first: with two row tiles K0 V0 K1 V1 ...; with one the
+    // scores run a block ahead: K0 K1 V0 K2 V1 ...
+    static __device__ __forceinline__ int k_at(int j) { return TILES == 2 || j == 0 ? j * PER_BLOCK : j * KC + (j - 1) * VC; }
+    static __device__ __forceinline__ int v_at(int j, int count) {
+        return TILES == 2 ? j * PER_BLOCK + KC : (j + 2 < count ? j + 2 : count) * KC + j * VC;
+    }
+};
+
+__device__ __forceinline__ uint32_t slot_of(long long seq, int nslot) { return (uint32_t)(seq % nslot); }
+
+template <int D>
+__global__ void __launch_bounds__(Chunk<D>::THREADS, 1)
+paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
+    using C = Chunk<D>;
+    constexpr int NS = C::NSLOT;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t s_q = base, s_ring = base + C::TILES * C::Q_TILE;
+    const uint32_t bars = s_ring + NS * kSlot;
+    uint8_t* tail = gen + C::TILES * C::Q_TILE + NS * kSlot;
+    auto full = [&](uint32_t s) { return bars + 8u * s; };
+    auto empty = [&](uint32_t s) { return bars + 8u * (NS + s); };
+    // per row tile (S and P: per score buffer)
+    auto s_full = [&](int t) { return bars + 8u * (2 * NS + t); };
+    auto p_full = [&](int t) { return bars + 8u * (2 * NS + 2 + t); };
+    auto o_done = [&](int t) { return bars + 8u * (2 * NS + 4 + t); };
+    auto q_full = [&](int t) { return bars + 8u * (2 * NS + 6 + t); };
+    const uint32_t drained = bars + 8u * (2 * NS + 8);  // only used when a wait has given up
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * C::BARS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
+    Walk* start = reinterpret_cast<Walk*>(tail + 8 * C::BARS + 16);
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NS; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(s_full(t), 1);
+            mbar_init(p_full(t), 4);
+            mbar_init(o_done(t), 1);
+            mbar_init(q_full(t), 4);
+        }
+        mbar_init(drained, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tensormap(&k_map);
+        prefetch_tensormap(&v_map);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+        tmem_relinquish();
+    }
+    find_range<C::THREADS>(a, kBK, C::ROWS, blockIdx.x, gridDim.x, start);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    Walk walk = *start;
+    Item it;
+    bool ok = true;
+    long long seq = 0;                                  // ring slots of the items before this one
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------------------ K and V
+        const int kbox = 1 << min(a.shift, 7), vbox = min(1 << a.shift, C::VKEYS);
+        while (next_item(a, walk, C::ROWS, kBK, it)) {
+            const int n = it.li.n, count = it.b1 - it.b0;
+            const int entries = (int)(((unsigned)n + (1u << a.shift) - 1u) >> a.shift);
+            const int32_t* tab = a.table + (size_t)it.list * a.max_pages;
+            auto entry = [&](int e) {
+                int page = 0;
+                if (e < entries) {
+                    page = tab[e];
+                    if ((unsigned)page >= (unsigned)a.n_pages) {
+                        a.status[1] = (int)EA_ERR_PAGES;
+                        page = 0;
+                    }
+                }
+                return page;
+            };
+            // table entries ride in registers: 32 from `win`, 32 after them (the next K block may lie there), 32 ahead
+            int win = (int)(((long long)it.b0 * kBK) >> a.shift) & ~31;
+            int e0 = entry(win + lane), e1 = entry(win + 32 + lane), e2 = entry(win + 64 + lane);
+            // `rows` keys from key0 into one slot; boxes of `box` keys; channels 64 c .. (K) or all of them (V)
+            auto load = [&](long long at, bool is_v, int c, int key0, int rows, int box) {
+                const uint32_t s = slot_of(at, NS), use = (uint32_t)(at / NS);
+                if (ok) ok = mbar_wait(empty(s), (use & 1) ^ 1, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) return;
+                const int rest = n - key0;
+                int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
+                const int wide = is_v ? D / 64 : 1;                           // boxes across the channels
+                if (lane == 0) mbar_arrive_expect_tx(full(s), (uint32_t)(act * box * 128 * wide));
+                __syncwarp();
+                const uint32_t dst = s_ring + s * kSlot;
+                const int boxes = act * wide;
+                for (int i0 = 0; i0 < boxes; i0 += 32) {
+                    const int i = i0 + lane, sub = i / wide, ch = is_v ? i % wide : c;
+                    const int key = key0 + sub * box, e = (key >> a.shift) - win;
+                    const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
+                    if (i < boxes) {
+                        const uint32_t to = dst + (uint32_t)((is_v ? ch * rows * 128 : 0) + sub * box * 128);
+                        tma_load_3d(to, is_v ? &v_map : &k_map, full(s), ch * 64, key & ((1 << a.shift) - 1), e < 32 ? p0 : p1);
+                    }
+                }
+            };
+            auto load_k = [&](int j) {
+                for (int c = 0; c < C::KC; ++c) load(seq + C::k_at(j) + c, false, c, (it.b0 + j) * kBK, kBK, kbox);
+            };
+            for (int j = 0; j < count; ++j) {
+                const int at = (int)(((long long)(it.b0 + j) * kBK) >> a.shift);
+                if (at >= win + 32) {
+                    win += 32;
+                    e0 = e1;
+                    e1 = e2;
+                    e2 = entry(win + 64 + lane);
+                }
+                if (C::TILES == 2 || j == 0) load_k(j);
+                if (C::TILES == 1 && j + 1 < count) load_k(j + 1);
+                for (int c = 0; c < C::VC; ++c)
+                    load(seq + C::v_at(j, count) + c, true, 0, (it.b0 + j) * kBK + c * C::VKEYS, C::VKEYS, vbox);
+            }
+            seq += (long long)count * C::PER_BLOCK;
+        }
+        if (!ok && lane == 0)
+            for (int s = 0; s < NS; ++s) {              // copies in flight land before the shared memory goes away
+                mbar_drain(full(s), 0);
+                mbar_drain(full(s), 1);
+            }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            const uint32_t idesc_s = umma_idesc_bf16_m128(kBK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
+            uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};  // phases of the barriers seen so far
+            auto scores = [&](int t, int buf, int j, bool first, bool last) {
+                // S of row tile t in buffer buf; first / last: of the row tiles that read this K block
+                for (int c = 0; c < C::KC; ++c) {
+                    const long long at = seq + C::k_at(j) + c;
+                    const uint32_t s = slot_of(at, NS);
+                    if (first && ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
+                    if (!ok) continue;
+                    tc_fence_after_sync();
+                    const uint32_t qa = s_q + t * C::Q_TILE + c * 16384u, ka = s_ring + s * kSlot;
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        umma_bf16(tmem + buf * 128, umma_desc_k_sw128(qa + ks * 32), umma_desc_k_sw128(ka + ks * 32), idesc_s,
+                                  (c | ks) ? 1u : 0u);
+                    if (last) umma_commit(empty(s));
+                }
+                if (ok) umma_commit(s_full(buf));
+            };
+            auto product = [&](int t, int buf, int j, int count, bool first, bool last) {
+                if (ok) ok = mbar_wait(p_full(buf), n_p[buf] & 1, abort_flag);
+                ++n_p[buf];
+                for (int c = 0; c < C::VC; ++c) {
+                    const long long at = seq + C::v_at(j, count) + c;
+                    const uint32_t s = slot_of(at, NS);
+                    if (first && ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
+                    if (!ok) continue;
+                    tc_fence_after_sync();
+                    const uint32_t va = s_ring + s * kSlot;
+#pragma unroll
+                    for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+                        umma_bf16_ts(tmem + C::O_COL + t * D, tmem + buf * 128 + (c * C::VKEYS + ks * 16) / 2,
+                                     umma_desc_mn_sw128(va + ks * 2048, C::VKEYS * 128), idesc_o, (j | c | ks) ? 1u : 0u);
+                    if (last) umma_commit(empty(s));
+                }
+                if (ok) umma_commit(o_done(t));
+            };
+            while (next_item(a, walk, C::ROWS, kBK, it)) {
+                const int count = it.b1 - it.b0;
+                const long long rows = (long long)it.li.rows_tok * a.G - (long long)it.tile * C::ROWS;
+                const int nt = C::TILES == 2 && rows > 128 ? 2 : 1;
+                for (int t = 0; t < nt; ++t) {
+                    if (ok) ok = mbar_wait(q_full(t), n_q[t] & 1, abort_flag);
+                    ++n_q[t];
+                }
+                if (C::TILES == 2) {
+                    for (int t = 0; t < nt; ++t) scores(t, t, 0, t == 0, t == nt - 1);
+                    for (int j = 0; j < count; ++j)
+                        for (int t = 0; t < nt; ++t) {
+                            product(t, t, j, count, t == 0, t == nt - 1);
+                            if (j + 1 < count) scores(t, t, j + 1, t == 0, t == nt - 1);
+                        }
+                } else {
+                    scores(0, 0, 0, true, true);
+                    if (count > 1) scores(0, 1, 1, true, true);
+                    for (int j = 0; j < count; ++j) {
+                        product(0, j & 1, j, count, true, true);
+                        if (j + 2 < count) scores(0, j & 1, j + 2, true, true);
+                    }
+                }
+                seq += (long long)count * C::PER_BLOCK;
+            }
+            if (!ok) {                                  // MMAs in flight end before the tensor memory goes back
+                umma_commit(drained);
+                mbar_drain(drained, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------------------ softmax, one row per thread
+        const int t = (warp - 2) / 4, quarter = warp & 3;
+        const int row = quarter * 32 + lane;            // tensor-memory lanes follow warp % 4
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t o_col = tmem + lanes + C::O_COL + t * D;
+        uint32_t n_s[2] = {0, 0}, n_o = 0;
+        const float sign = a.scale_log2 < 0.f ? -1.f : 1.f;
+        const float scale = fabsf(a.scale_log2);        // the queries take the sign (exact), so that max(c S) = c max(S)
+        while (next_item(a, walk, C::ROWS, kBK, it)) {
+            const ListInfo& li = it.li;
+            const int count = it.b1 - it.b0;
+            const long long live_rows = (long long)li.rows_tok * a.G - (long long)it.tile * C::ROWS;
+            const int nt = C::TILES == 2 && live_rows > 128 ? 2 : 1;
+            if (t >= nt) {
+                seq += (long long)count * C::PER_BLOCK;
+                continue;
+            }
+            // ---- queries: 16 bytes per thread and step, rows without a query are zero
+            const int head0 = (it.list % a.Hkv) * a.G;
+            const int tid = threadIdx.x - 64 - t * 128;
+            const long long row0 = (long long)it.tile * C::ROWS + t * 128;
+            constexpr int PIECES = D / 8;
+#pragma unroll 4
+            for (int i = tid; i < 128 * PIECES; i += 128) {
+                const int r = i / PIECES, piece = i % PIECES;
+                const long long pr = row0 + r;
+                const int tok = (int)(pr / a.G), h = head0 + (int)(pr % a.G);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (tok < li.rows_tok) {
+                    v = *reinterpret_cast<const uint4*>(a.q + (long long)(li.q0 + tok) * a.q_stride + (long long)h * D + piece * 8);
+                    if (sign < 0.f) {
+                        v.x ^= 0x80008000u;
+                        v.y ^= 0x80008000u;
+                        v.z ^= 0x80008000u;
+                        v.w ^= 0x80008000u;
+                    }
+                }
+                sts128(s_q + t * C::Q_TILE + (piece / 8) * 16384u + r * 128u + (((piece % 8) * 16u) ^ ((r & 7) * 16u)), v);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full(t));
+
+            const long long pr = row0 + row;
+            const int tok = (int)(pr / a.G), head = head0 + (int)(pr % a.G);
+            const bool live = tok < li.rows_tok;
+            const int lim = live ? limit_of(li, a, tok) : 0;
+            // keys that every row of the tile sees
+            const int seen = limit_of(li, a, (int)(row0 / a.G));
+            float m = -INFINITY, l = 0.f;
+            for (int j = 0; j < count; ++j) {
+                const int key0 = (it.b0 + j) * kBK;
+                const int buf = C::TILES == 2 ? t : j & 1;
+                if (ok) ok = mbar_wait(s_full(buf), n_s[buf] & 1, abort_flag);
+                ++n_s[buf];
+                ok = __all_sync(0xffffffffu, ok);
+                if (key0 + kBK > li.n && t == 0) {
+                    // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN:
+                    // they become zero before the product is let go.  (A parity tells two neighbouring phases apart: with
+                    // scores a block ahead, the slots' earlier use is only known to be over when the product before is.)
+                    if (C::TILES == 1 && j > 0 && ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
+                    for (int c = 0; c < C::VC; ++c) {
+                        const long long at = seq + C::v_at(j, count) + c;
+                        const uint32_t s = slot_of(at, NS);
+                        const int from = max(0, li.n - key0 - c * C::VKEYS);
+                        if (from >= C::VKEYS) continue;
+                        if (ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
+                        const int todo = (C::VKEYS - from) * PIECES;
+                        for (int i = tid; i < todo; i += 128) {
+                            const int r = from + i / PIECES, piece = i % PIECES;
+                            sts128(s_ring + s * kSlot + (piece / 8) * (C::VKEYS * 128u) + r * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
+                        }
+                    }
+                    fence_proxy_async_smem();
+                }
+                __syncwarp();
+                tc_fence_after_sync();
+                const uint32_t s_col = tmem + lanes + buf * 128;
+                uint32_t x[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld_x32(s_col + i * 32, x[i]);
+                tmem_ld_wait();
+                if (key0 + kBK > seen) {
+                    const int local = lim - key0;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i >= local) x[i / 32][i % 32] = 0xff800000u;
+                }
+                float top[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    top[i] = __uint_as_float(x[i][0]);
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(x[i][e]));
+                }
+                const float raw = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                const float m_blk = raw == -INFINITY ? -INFINITY : raw * scale;
+                bool move = false;
+                float f = 1.f;
+                if (m == -INFINITY) {
+                    m = m_blk;                          // nothing seen so far: sum and output are zero
+                } else if (m_blk > m + kRescale) {
+                    f = ex2(m - m_blk);
+                    l *= f;
+                    m = m_blk;
+                    move = true;
+                }
+                if (__any_sync(0xffffffffu, move)) {
+                    // (j > 0: m was finite.)  The product of the block before must have ended.
+                    if (ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    tc_fence_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld_x32(o_col + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st_x32(o_col + c, o);
+                    }
+                }
+                const float z = m == -INFINITY ? 0.f : m;
+                const float2 c2 = make_float2(scale, scale), z2 = make_float2(-z, -z);
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                const bool masked = key0 + kBK > seen;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
+                        // (a scale of zero makes NaN of a masked score)
+                        if (masked) {
+                            if (x[i][e] == 0xff800000u) y.x = -INFINITY;
+                            if (x[i][e + 1] == 0xff800000u) y.y = -INFINITY;
+                        }
+                        y.x = ex2(y.x);
+                        y.y = ex2(y.y);
+                        sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
+                        p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
+                    }
+                    tmem_st_x16(s_col + i * 16, p);
+                }
+                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full(buf));
+            }
+            // ---- output
+            n_o += (uint32_t)count;
+            // (a parity tells two neighbouring phases apart.  With scores a block ahead, all that is known here is that
+            // the product of two blocks before the last has ended, so its successor is waited for on its own)
+            if (C::TILES == 1 && count > 1 && ok) ok = mbar_wait(o_done(t), (n_o - 2) & 1, abort_flag);
+            if (ok) ok = mbar_wait(o_done(t), (n_o - 1) & 1, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after_sync();
+            const bool whole = it.b0 == 0 && it.b1 == it.blocks;
+            const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+            const size_t at = (size_t)(li.q0 + tok) * a.Hq + head;
+            const size_t part = ((size_t)2 * blockIdx.x + (it.first ? 0 : 1)) * C::ROWS + t * 128 + row;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_ld_x32(o_col + c, o);
+                tmem_ld_wait();
+                if (live && whole) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 v;
+                        v.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                        v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                        v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                        v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                        *reinterpret_cast<uint4*>(a.out + at * D + c + e) = v;
+                    }
+                } else if (live) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4*>(a.part_o + part * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+                __syncwarp();
+            }
+            if (live) {
+                if (whole) {
+                    if (a.lse) a.lse[at] = lse_of(m, l);
+                } else {
+                    *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(m, l);
+                }
+            }
+            // (the loads above precede this warp's next arrival, which lets the next item's product overwrite O)
+            tc_fence_before_sync();
+            seq += (long long)count * C::PER_BLOCK;
+        }
+    }
+
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, 512);
+    }
+    if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
+}
+
+template <int D>
+ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& args, const void* k_pages, const void* v_pages, cudaStream_t st) {
+    using C = Chunk<D>;
+    AttnArgs a = args;
+    const int ctas = ctx->sm_count < kPagedMaxCtas ? ctx->sm_count : kPagedMaxCtas;
+    a.part_o = static_cast<float*>(ctx->workspace);
+    a.part_ml = a.part_o + (size_t)2 * kPagedMaxCtas * C::ROWS * D;
+    CUtensorMap k_map, v_map;
+    const uint32_t kbox = (uint32_t)s.page_rows, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
+    if (!ea_paged_map(ctx, s, k_pages, kbox, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, &v_map)) return EA_ERR_CUDA;
+    auto kernel = paged_chunk_kernel<D>;
+    EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
+    ea_count_launches(ctx, 1);
+    ea_status err = EA_CHECK_LAUNCH();
+    if (err != EA_OK) return err;
+    return ea_launch_paged_combine(ctx, s, a, C::ROWS, kBK, ctas, st);
+}
+
+}  // namespace
+
+size_t ea_paged_chunk_ws_floats(int d) { return (size_t)2 * kPagedMaxCtas * (d == 256 ? 128 : 256) * (d + 2); }
+
+ea_status ea_launch_paged_chunk(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, const void* k_pages, const void* v_pages,
+                                cudaStream_t st) {
+    return s.head_dim == 64    ? launch<64>(ctx, s, a, k_pages, v_pages, st)
+           : s.head_dim == 128 ? launch<128>(ctx, s, a, k_pages, v_pages, st)
+                               : launch<256>(ctx, s, a, k_pages, v_pages, st);
+}
