@@ -319,47 +319,74 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
 }
 
-// Joins the partial results of row tiles (ROWS rows) that several CTAs shared: one CTA per (tile, list).
+// Joins the partial results of row tiles (ROWS rows) that several CTAs shared: one CTA per (tile, 16 of its rows, list).
+// First a warp per row turns the parts' maxima and sums into weights, then every thread adds 4 channels of a row over
+// the parts, in the order of the keys.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, int BK, int ctas) {
-    const int r = blockIdx.y, tile = blockIdx.x;
+    __shared__ float weight[16][kPagedMaxCtas];
+    constexpr int GROUPS = ROWS / 16;
+    const int r = blockIdx.y, tile = blockIdx.x / GROUPS, row0 = blockIdx.x % GROUPS * 16;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const ListInfo li = list_info(a, r, false);
-    if (tile >= tiles_of(li, a, ROWS)) return;
-    // units before this list, and in all
+    const long long rows_left = (long long)li.rows_tok * a.G - ((long long)tile * ROWS + row0);
+    if (rows_left <= 0) return;
+    const int live = rows_left < 16 ? (int)rows_left : 16;
     long long before, total;
     count_units<128>(a, BK, ROWS, r, &before, &total);
     long long u0 = before;
     for (int t = 0; t < tile; ++t) u0 += tile_blocks(li, a, t, ROWS, BK);
     const long long u1 = u0 + tile_blocks(li, a, tile, ROWS, BK);
-    const int c0 = owner_of(u0, total, ctas), c1 = owner_of(u1 - 1, total, ctas);
-    if (c0 == c1) return;
-    const int slot0 = u0 > range_begin(c0, total, ctas) ? 2 * c0 + 1 : 2 * c0;
-    for (int i = threadIdx.x; i < ROWS * (D / 4); i += 128) {
-        const int row = i / (D / 4), col = i % (D / 4);
-        const int pr = tile * ROWS + row, tok = pr / a.G;
-        if (tok >= li.rows_tok) break;
-        float m = -INFINITY;
-        for (int c = c0; c <= c1; ++c)
-            if (owns_some(c, total, ctas)) m = fmaxf(m, a.part_ml[((size_t)(c == c0 ? slot0 : 2 * c) * ROWS + row) * 2]);
-        const float z = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = c0; c <= c1; ++c) {
-            if (!owns_some(c, total, ctas)) continue;
-            const size_t at = (size_t)(c == c0 ? slot0 : 2 * c) * ROWS + row;
-            const float2 p = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-            const float f = ex2(p.x - z);
-            const float4 v = *reinterpret_cast<const float4*>(a.part_o + at * D + col * 4);
-            l += p.y * f;
-            o.x += v.x * f;
-            o.y += v.y * f;
-            o.z += v.z * f;
-            o.w += v.w * f;
+    const Division division(total, ctas);
+    const int c0 = division.owner(u0), c1 = division.owner(u1 - 1), parts = c1 - c0 + 1;
+    if (parts == 1) return;
+    // a CTA's first item is its part 0, its last part 1: only the tile's first CTA may have begun before it
+    const size_t p0 = ((size_t)2 * c0 + (u0 > division.begin(c0) ? 1 : 0)) * ROWS + row0;
+    const size_t p1 = (size_t)2 * (c0 + 1) * ROWS + row0;                   // part 1 of the tile; the next ones 2 ROWS on
+    for (int row = warp; row < live; row += 4) {
+        float m = -INFINITY, l = 0.f;
+        for (int p = lane; p < parts; p += 32) {
+            const float2 v = *reinterpret_cast<const float2*>(a.part_ml + ((p == 0 ? p0 : p1 + (size_t)(p - 1) * 2 * ROWS) + row) * 2);
+            weight[row][p] = v.x;
+            m = fmaxf(m, v.x);
         }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        const float z = m == -INFINITY ? 0.f : m;
+        for (int p = lane; p < parts; p += 32) {
+            const float f = ex2(weight[row][p] - z);
+            l += f * a.part_ml[((p == 0 ? p0 : p1 + (size_t)(p - 1) * 2 * ROWS) + row) * 2 + 1];
+            weight[row][p] = f;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-        const size_t at = (size_t)(li.q0 + tok) * a.Hq + (r % a.Hkv) * a.G + pr % a.G;
-        *reinterpret_cast<uint2*>(a.out + at * D + col * 4) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (a.lse && col == 0) a.lse[at] = lse_of(m, l);
+        for (int p = lane; p < parts; p += 32) weight[row][p] *= inv;
+        if (lane == 0 && a.lse) {
+            const long long pr = (long long)tile * ROWS + row0 + row;
+            a.lse[(size_t)(li.q0 + (int)(pr / a.G)) * a.Hq + (r % a.Hkv) * a.G + (int)(pr % a.G)] = lse_of(m, l);
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < live * (D / 4); i += 128) {
+        const int row = i / (D / 4), col = i % (D / 4) * 4;
+        const float* src = a.part_o + (p0 + row) * D + col;
+        const float* next = a.part_o + (p1 + row) * D + col;
+        float4 o = *reinterpret_cast<const float4*>(src);
+        const float w0 = weight[row][0];
+        o = make_float4(o.x * w0, o.y * w0, o.z * w0, o.w * w0);
+#pragma unroll 8
+        for (int p = 1; p < parts; ++p) {
+            const float w = weight[row][p];
+            const float4 v = *reinterpret_cast<const float4*>(next + (size_t)(p - 1) * 2 * ROWS * D);
+            o.x += v.x * w;
+            o.y += v.y * w;
+            o.z += v.z * w;
+            o.w += v.w * w;
+        }
+        const long long pr = (long long)tile * ROWS + row0 + row;
+        const size_t at = (size_t)(li.q0 + (int)(pr / a.G)) * a.Hq + (r % a.Hkv) * a.G + (int)(pr % a.G);
+        *reinterpret_cast<uint2*>(a.out + at * D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
     }
 }
 
@@ -399,7 +426,7 @@ bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages,
 }
 
 ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st) {
-    const dim3 grid((unsigned)(((long long)a.max_q * a.G + rows - 1) / rows), (unsigned)(s.n_seqs * s.n_kv_heads));
+    const dim3 grid((unsigned)(((long long)a.max_q * a.G + rows - 1) / rows * (rows / 16)), (unsigned)(s.n_seqs * s.n_kv_heads));
     const int d = s.head_dim;
     auto kernel = rows == 16    ? (d == 64 ? paged_combine_kernel<64, 16> : d == 128 ? paged_combine_kernel<128, 16> : paged_combine_kernel<256, 16>)
                   : rows == 128 ? paged_combine_kernel<256, 128>

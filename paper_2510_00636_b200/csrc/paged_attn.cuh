@@ -72,15 +72,18 @@ __device__ __forceinline__ long long list_units(const ListInfo& li, const AttnAr
     return u;
 }
 
-// CTA c of n takes units [c W / n, (c + 1) W / n) of the call's W units (unit: one key block of one row tile).
-__device__ __forceinline__ long long range_begin(int c, long long total, int ctas) { return (long long)c * total / ctas; }
-__device__ __forceinline__ int owner_of(long long unit, long long total, int ctas) {
-    return (int)(((unit + 1) * ctas - 1) / total);
-}
-// (fewer units than CTAs: some own none, and leave nothing behind)
-__device__ __forceinline__ bool owns_some(int c, long long total, int ctas) {
-    return range_begin(c, total, ctas) < range_begin(c + 1, total, ctas);
-}
+// The call's W units (unit: one key block of one row tile) in their order, divided among n CTAs: W / n each and one more
+// for the first W mod n, so that the owners of consecutive units are consecutive CTAs, none of them idle.
+struct Division {
+    long long each;
+    int extra;
+    __device__ __forceinline__ Division(long long total, int ctas) : each(total / ctas), extra((int)(total % ctas)) {}
+    __device__ __forceinline__ long long begin(int c) const { return c * each + (c < extra ? c : extra); }
+    __device__ __forceinline__ int owner(long long unit) const {
+        const long long wide = (each + 1) * extra;
+        return unit < wide ? (int)(unit / (each + 1)) : extra + (int)((unit - wide) / each);
+    }
+};
 
 // A CTA's share: where it begins, and how many units it has.
 struct Walk {
@@ -145,8 +148,8 @@ __device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int cta
         total += warp_sum[w];
     }
     long long at = before + inc - mine;
-    const long long first = total > 0 ? range_begin(cta, total, ctas) : 0;
-    const long long end = total > 0 ? range_begin(cta + 1, total, ctas) : 0;
+    const Division division(total, ctas);
+    const long long first = division.begin(cta), end = division.begin(cta + 1);
     if (tid == 0) {
         out->count = out->left = end - first;
         out->list = out->tile = out->block = 0;
@@ -221,6 +224,11 @@ __device__ __forceinline__ float ex2(float x) {
 // m: maximum of the scores in units of log 2, l: sum of 2^(score - m)
 __device__ __forceinline__ float lse_of(float m, float l) {
     return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;

@@ -34,21 +34,31 @@ template <int D> struct Chunk {
     static constexpr int PER_BLOCK = KC + VC;
     static constexpr uint32_t Q_TILE = 128u * D * 2;
     static constexpr int NSLOT = D == 64 ? 12 : 10;
-    static constexpr int THREADS = 64 + TILES * 128;
+    static constexpr int THREADS = 128 + TILES * 128;   // warps 0 (loads), 1 (MMA), two idle, then the softmax warps
+    // registers: 384 threads x 168 = 128 x 80 + 256 x 208 at most; 256 threads start with enough for everyone
+    static constexpr bool SPLIT = TILES == 2;
     static constexpr int BARS = 2 * NSLOT + 9;
     static constexpr int TAIL = BARS * 8 + 16 + (int)sizeof(Walk);
     static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)kSlot + TAIL;
     static constexpr uint32_t O_COL = 256;              // tensor memory: S (P) at 0 and 128, O from 256
     static_assert(SMEM + 1024 <= 232448, "a CTA's shared memory, with room for static arrays");
-    // Order of the blocks in the ring, in slots after the item's first: with two row tiles K0 V0 K1 V1 ...; with one the
-    // scores run a block ahead: K0 K1 V0 K2 V1 ...
-    static __device__ __forceinline__ int k_at(int j) { return TILES == 2 || j == 0 ? j * PER_BLOCK : j * KC + (j - 1) * VC; }
-    static __device__ __forceinline__ int v_at(int j, int count) {
-        return TILES == 2 ? j * PER_BLOCK + KC : (j + 2 < count ? j + 2 : count) * KC + j * VC;
-    }
+    // Scores run LEAD blocks ahead of the product.  Order of the blocks in the ring: with two row tiles K0 V0 K1 V1 ...,
+    // with one K0 K1 V0 K2 V1 ...
+    static constexpr int LEAD = TILES == 2 ? 1 : 2;
+    // where block j's V begins, in slots after the item's first
+    static __device__ __forceinline__ int v_at(int j, int count) { return (j + LEAD < count ? j + LEAD : count) * KC + j * VC; }
 };
 
-__device__ __forceinline__ uint32_t slot_of(long long seq, int nslot) { return (uint32_t)(seq % nslot); }
+// A place in the ring: slot, and the parity of its use.
+struct Ring {
+    uint32_t slot, phase;
+    __device__ __forceinline__ void next(int nslot) {
+        if (++slot == (uint32_t)nslot) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 template <int D>
 __global__ void __launch_bounds__(Chunk<D>::THREADS, 1)
@@ -103,10 +113,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     Walk walk = *start;
     Item it;
     bool ok = true;
-    long long seq = 0;                                  // ring slots of the items before this one
 
+    if (warp < 4) {
+    if (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 0) {
         // ------------------------------------------------------------------------------ K and V
+        Ring ring = {0, 0};
         const int kbox = 1 << min(a.shift, 7), vbox = min(1 << a.shift, C::VKEYS);
         while (next_item(a, walk, C::ROWS, kBK, it)) {
             const int n = it.li.n, count = it.b1 - it.b0;
@@ -126,46 +138,44 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             // table entries ride in registers: 32 from `win`, 32 after them (the next K block may lie there), 32 ahead
             int win = (int)(((long long)it.b0 * kBK) >> a.shift) & ~31;
             int e0 = entry(win + lane), e1 = entry(win + 32 + lane), e2 = entry(win + 64 + lane);
-            // `rows` keys from key0 into one slot; boxes of `box` keys; channels 64 c .. (K) or all of them (V)
-            auto load = [&](long long at, bool is_v, int c, int key0, int rows, int box) {
-                const uint32_t s = slot_of(at, NS), use = (uint32_t)(at / NS);
-                if (ok) ok = mbar_wait(empty(s), (use & 1) ^ 1, abort_flag);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) return;
-                const int rest = n - key0;
-                int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
-                const int wide = is_v ? D / 64 : 1;                           // boxes across the channels
-                if (lane == 0) mbar_arrive_expect_tx(full(s), (uint32_t)(act * box * 128 * wide));
-                __syncwarp();
-                const uint32_t dst = s_ring + s * kSlot;
-                const int boxes = act * wide;
-                for (int i0 = 0; i0 < boxes; i0 += 32) {
-                    const int i = i0 + lane, sub = i / wide, ch = is_v ? i % wide : c;
-                    const int key = key0 + sub * box, e = (key >> a.shift) - win;
-                    const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
-                    if (i < boxes) {
-                        const uint32_t to = dst + (uint32_t)((is_v ? ch * rows * 128 : 0) + sub * box * 128);
-                        tma_load_3d(to, is_v ? &v_map : &k_map, full(s), ch * 64, key & ((1 << a.shift) - 1), e < 32 ? p0 : p1);
-                    }
-                }
-            };
-            auto load_k = [&](int j) {
-                for (int c = 0; c < C::KC; ++c) load(seq + C::k_at(j) + c, false, c, (it.b0 + j) * kBK, kBK, kbox);
-            };
-            for (int j = 0; j < count; ++j) {
-                const int at = (int)(((long long)(it.b0 + j) * kBK) >> a.shift);
+            // block by block: the K chunks of block j + LEAD - 1, then the V chunks of block j
+            for (int j = 1 - C::LEAD; j < count; ++j) {
+                const int at = (int)(((long long)(it.b0 + max(j, 0)) * kBK) >> a.shift);
                 if (at >= win + 32) {
                     win += 32;
                     e0 = e1;
                     e1 = e2;
                     e2 = entry(win + 64 + lane);
                 }
-                if (C::TILES == 2 || j == 0) load_k(j);
-                if (C::TILES == 1 && j + 1 < count) load_k(j + 1);
-                for (int c = 0; c < C::VC; ++c)
-                    load(seq + C::v_at(j, count) + c, true, 0, (it.b0 + j) * kBK + c * C::VKEYS, C::VKEYS, vbox);
+#pragma unroll 1
+                for (int i = 0; i < C::PER_BLOCK; ++i) {
+                    const bool is_v = i >= C::KC;
+                    const int jj = is_v ? j : j + C::LEAD - 1, c = is_v ? i - C::KC : i;
+                    if (jj < 0 || jj >= count) continue;
+                    // `rows` keys from key0 into one slot in boxes of `box`; channels 64 c .. (K) or all of them (V)
+                    const int key0 = (it.b0 + jj) * kBK + (is_v ? c * C::VKEYS : 0);
+                    const int rows = is_v ? C::VKEYS : kBK, box = is_v ? vbox : kbox, wide = is_v ? D / 64 : 1;
+                    if (ok) ok = mbar_wait(empty(ring.slot), ring.phase ^ 1, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) continue;
+                    const int rest = n - key0;
+                    const int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
+                    if (lane == 0) mbar_arrive_expect_tx(full(ring.slot), (uint32_t)(act * box * 128 * wide));
+                    __syncwarp();
+                    const uint32_t dst = s_ring + ring.slot * kSlot;
+                    const int boxes = act * wide;
+                    for (int x0 = 0; x0 < boxes; x0 += 32) {
+                        const int x = x0 + lane, sub = x / wide, ch = is_v ? x % wide : c;
+                        const int key = key0 + sub * box, e = (key >> a.shift) - win;
+                        const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
+                        if (x < boxes) {
+                            const uint32_t to = dst + (uint32_t)((is_v ? ch * rows * 128 : 0) + sub * box * 128);
+                            tma_load_3d(to, is_v ? &v_map : &k_map, full(ring.slot), ch * 64, key & ((1 << a.shift) - 1), e < 32 ? p0 : p1);
+                        }
+                    }
+                    ring.next(NS);
+                }
             }
-            seq += (long long)count * C::PER_BLOCK;
         }
         if (!ok && lane == 0)
             for (int s = 0; s < NS; ++s) {              // copies in flight land before the shared memory goes away
@@ -178,41 +188,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         if (lane == 0) {
             const uint32_t idesc_s = umma_idesc_bf16_m128(kBK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
             uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};  // phases of the barriers seen so far
-            auto scores = [&](int t, int buf, int j, bool first, bool last) {
-                // S of row tile t in buffer buf; first / last: of the row tiles that read this K block
-                for (int c = 0; c < C::KC; ++c) {
-                    const long long at = seq + C::k_at(j) + c;
-                    const uint32_t s = slot_of(at, NS);
-                    if (first && ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
-                    if (!ok) continue;
-                    tc_fence_after_sync();
-                    const uint32_t qa = s_q + t * C::Q_TILE + c * 16384u, ka = s_ring + s * kSlot;
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        umma_bf16(tmem + buf * 128, umma_desc_k_sw128(qa + ks * 32), umma_desc_k_sw128(ka + ks * 32), idesc_s,
-                                  (c | ks) ? 1u : 0u);
-                    if (last) umma_commit(empty(s));
-                }
-                if (ok) umma_commit(s_full(buf));
-            };
-            auto product = [&](int t, int buf, int j, int count, bool first, bool last) {
-                if (ok) ok = mbar_wait(p_full(buf), n_p[buf] & 1, abort_flag);
-                ++n_p[buf];
-                for (int c = 0; c < C::VC; ++c) {
-                    const long long at = seq + C::v_at(j, count) + c;
-                    const uint32_t s = slot_of(at, NS);
-                    if (first && ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
-                    if (!ok) continue;
-                    tc_fence_after_sync();
-                    const uint32_t va = s_ring + s * kSlot;
-#pragma unroll
-                    for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-                        umma_bf16_ts(tmem + C::O_COL + t * D, tmem + buf * 128 + (c * C::VKEYS + ks * 16) / 2,
-                                     umma_desc_mn_sw128(va + ks * 2048, C::VKEYS * 128), idesc_o, (j | c | ks) ? 1u : 0u);
-                    if (last) umma_commit(empty(s));
-                }
-                if (ok) umma_commit(o_done(t));
-            };
+            Ring ring = {0, 0}, k_ring = {0, 0}, v_ring = {0, 0};
             while (next_item(a, walk, C::ROWS, kBK, it)) {
                 const int count = it.b1 - it.b0;
                 const long long rows = (long long)it.li.rows_tok * a.G - (long long)it.tile * C::ROWS;
@@ -221,22 +197,55 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     if (ok) ok = mbar_wait(q_full(t), n_q[t] & 1, abort_flag);
                     ++n_q[t];
                 }
-                if (C::TILES == 2) {
-                    for (int t = 0; t < nt; ++t) scores(t, t, 0, t == 0, t == nt - 1);
-                    for (int j = 0; j < count; ++j)
-                        for (int t = 0; t < nt; ++t) {
-                            product(t, t, j, count, t == 0, t == nt - 1);
-                            if (j + 1 < count) scores(t, t, j + 1, t == 0, t == nt - 1);
+#pragma unroll 1
+                for (int j = -C::LEAD; j < count; ++j)
+#pragma unroll 1
+                    for (int t = 0; t < nt; ++t) {
+                        // (both row tiles read a block: the first waits for its slots, the last gives them back)
+                        const bool first = t == 0, last = t == nt - 1;
+                        const int buf = C::TILES == 2 ? t : j & 1;
+                        if (j >= 0) {                   // O += P(j) V(j)
+                            if (ok) ok = mbar_wait(p_full(buf), n_p[buf] & 1, abort_flag);
+                            ++n_p[buf];
+                            Ring r = first ? ring : v_ring;
+                            if (first) v_ring = ring;
+#pragma unroll 1
+                            for (int c = 0; c < C::VC; ++c) {
+                                if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
+                                if (ok) {
+                                    tc_fence_after_sync();
+                                    const uint64_t vd = umma_desc_mn_sw128(s_ring + r.slot * kSlot, C::VKEYS * 128);
+                                    const uint32_t pa = tmem + buf * 128 + c * (C::VKEYS / 2);
+#pragma unroll
+                                    for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+                                        umma_bf16_ts(tmem + C::O_COL + t * D, pa + ks * 8, vd + ks * (2048 >> 4), idesc_o, (j | c | ks) ? 1u : 0u);
+                                    if (last) umma_commit(empty(r.slot));
+                                }
+                                r.next(NS);
+                            }
+                            if (first) ring = r;
+                            if (ok) umma_commit(o_done(t));
                         }
-                } else {
-                    scores(0, 0, 0, true, true);
-                    if (count > 1) scores(0, 1, 1, true, true);
-                    for (int j = 0; j < count; ++j) {
-                        product(0, j & 1, j, count, true, true);
-                        if (j + 2 < count) scores(0, j & 1, j + 2, true, true);
+                        if (j + C::LEAD < count) {      // S(j + LEAD) = Q K^T, over the P just used
+                            Ring r = first ? ring : k_ring;
+                            if (first) k_ring = ring;
+#pragma unroll 1
+                            for (int c = 0; c < C::KC; ++c) {
+                                if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
+                                if (ok) {
+                                    tc_fence_after_sync();
+                                    const uint64_t qd = umma_desc_k_sw128(s_q + t * C::Q_TILE + c * 16384u), kd = umma_desc_k_sw128(s_ring + r.slot * kSlot);
+#pragma unroll
+                                    for (int ks = 0; ks < 4; ++ks)
+                                        umma_bf16(tmem + buf * 128, qd + ks * 2, kd + ks * 2, idesc_s, (c | ks) ? 1u : 0u);
+                                    if (last) umma_commit(empty(r.slot));
+                                }
+                                r.next(NS);
+                            }
+                            if (first) ring = r;
+                            if (ok) umma_commit(s_full(buf));
+                        }
                     }
-                }
-                seq += (long long)count * C::PER_BLOCK;
             }
             if (!ok) {                                  // MMAs in flight end before the tensor memory goes back
                 umma_commit(drained);
@@ -244,15 +253,20 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
         }
         __syncwarp();
+    }
     } else {
+        if (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ------------------------------------------------------------------------------ softmax, one row per thread
-        const int t = (warp - 2) / 4, quarter = warp & 3;
+        const int t = (warp - 4) / 4, quarter = warp & 3;
         const int row = quarter * 32 + lane;            // tensor-memory lanes follow warp % 4
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t o_col = tmem + lanes + C::O_COL + t * D;
         uint32_t n_s[2] = {0, 0}, n_o = 0;
+        long long seq = 0;                              // ring slots of the items before this one
         const float sign = a.scale_log2 < 0.f ? -1.f : 1.f;
-        const float scale = fabsf(a.scale_log2);        // the queries take the sign (exact), so that max(c S) = c max(S)
+        // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
+        // any score but does not make NaN of a masked one (-infinity)
+        const float scale = a.scale_log2 == 0.f ? 1e-37f : fabsf(a.scale_log2);
         while (next_item(a, walk, C::ROWS, kBK, it)) {
             const ListInfo& li = it.li;
             const int count = it.b1 - it.b0;
@@ -264,7 +278,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
             // ---- queries: 16 bytes per thread and step, rows without a query are zero
             const int head0 = (it.list % a.Hkv) * a.G;
-            const int tid = threadIdx.x - 64 - t * 128;
+            const int tid = threadIdx.x - 128 - t * 128;
             const long long row0 = (long long)it.tile * C::ROWS + t * 128;
             constexpr int PIECES = D / 8;
 #pragma unroll 4
@@ -308,7 +322,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     if (C::TILES == 1 && j > 0 && ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
                     for (int c = 0; c < C::VC; ++c) {
                         const long long at = seq + C::v_at(j, count) + c;
-                        const uint32_t s = slot_of(at, NS);
+                        const uint32_t s = (uint32_t)(at % NS);
                         const int from = max(0, li.n - key0 - c * C::VKEYS);
                         if (from >= C::VKEYS) continue;
                         if (ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
@@ -338,10 +352,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 for (int i = 0; i < 4; ++i) {
                     top[i] = __uint_as_float(x[i][0]);
 #pragma unroll
-                    for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(x[i][e]));
+                    for (int e = 1; e < 31; e += 2) top[i] = max3(top[i], __uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1]));
+                    top[i] = fmaxf(top[i], __uint_as_float(x[i][31]));
                 }
-                const float raw = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                const float m_blk = raw == -INFINITY ? -INFINITY : raw * scale;
+                const float m_blk = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
                 bool move = false;
                 float f = 1.f;
                 if (m == -INFINITY) {
@@ -370,18 +384,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 const float z = m == -INFINITY ? 0.f : m;
                 const float2 c2 = make_float2(scale, scale), z2 = make_float2(-z, -z);
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                const bool masked = key0 + kBK > seen;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uint32_t p[16];
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
-                        // (a scale of zero makes NaN of a masked score)
-                        if (masked) {
-                            if (x[i][e] == 0xff800000u) y.x = -INFINITY;
-                            if (x[i][e + 1] == 0xff800000u) y.y = -INFINITY;
-                        }
                         y.x = ex2(y.x);
                         y.y = ex2(y.y);
                         sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
