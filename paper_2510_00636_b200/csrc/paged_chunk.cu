@@ -83,7 +83,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
     Walk* start = reinterpret_cast<Walk*>(tail + 8 * C::BARS + 16);
 
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
             mbar_init(full(s), 1);
@@ -185,72 +185,77 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------------------------------------ MMA issuer
-        if (lane == 0) {
-            const uint32_t idesc_s = umma_idesc_bf16_m128(kBK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
-            uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};  // phases of the barriers seen so far
-            Ring ring = {0, 0}, k_ring = {0, 0}, v_ring = {0, 0};
-            while (next_item(a, walk, C::ROWS, kBK, it)) {
-                const int count = it.b1 - it.b0;
-                const long long rows = (long long)it.li.rows_tok * a.G - (long long)it.tile * C::ROWS;
-                const int nt = C::TILES == 2 && rows > 128 ? 2 : 1;
+        // The whole warp runs this loop in step, and one lane issues (see umma_bf16_warp).
+        const uint32_t leader = elect_one();
+        const uint32_t idesc_s = umma_idesc_bf16_m128(kBK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
+        const uint64_t q_desc = umma_desc_k_sw128(s_q), k_desc = umma_desc_k_sw128(s_ring);
+        const uint64_t v_desc = umma_desc_mn_sw128(s_ring, C::VKEYS * 128);
+        uint32_t p_phase = 0, q_phase = 0;              // bit t: parity of the next phase of p_full(t), q_full(t)
+        Ring ring = {0, 0}, k_ring = {0, 0}, v_ring = {0, 0};
+        while (next_item(a, walk, C::ROWS, kBK, it)) {
+            const int count = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
+            const long long rows = (long long)it.li.rows_tok * a.G - (long long)it.tile * C::ROWS;
+            const int nt = __shfl_sync(0xffffffffu, C::TILES == 2 && rows > 128 ? 2 : 1, 0);
+            for (int t = 0; t < nt; ++t) {
+                if (ok) ok = mbar_wait(q_full(t), (q_phase >> t) & 1, abort_flag);
+                q_phase ^= 1u << t;
+            }
+#pragma unroll 1
+            for (int j = -C::LEAD; j < count; ++j)
+#pragma unroll 1
                 for (int t = 0; t < nt; ++t) {
-                    if (ok) ok = mbar_wait(q_full(t), n_q[t] & 1, abort_flag);
-                    ++n_q[t];
-                }
-#pragma unroll 1
-                for (int j = -C::LEAD; j < count; ++j)
-#pragma unroll 1
-                    for (int t = 0; t < nt; ++t) {
-                        // (both row tiles read a block: the first waits for its slots, the last gives them back)
-                        const bool first = t == 0, last = t == nt - 1;
-                        const int buf = C::TILES == 2 ? t : j & 1;
-                        if (j >= 0) {                   // O += P(j) V(j)
-                            if (ok) ok = mbar_wait(p_full(buf), n_p[buf] & 1, abort_flag);
-                            ++n_p[buf];
-                            Ring r = first ? ring : v_ring;
-                            if (first) v_ring = ring;
-#pragma unroll 1
-                            for (int c = 0; c < C::VC; ++c) {
-                                if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
-                                if (ok) {
-                                    tc_fence_after_sync();
-                                    const uint64_t vd = umma_desc_mn_sw128(s_ring + r.slot * kSlot, C::VKEYS * 128);
-                                    const uint32_t pa = tmem + buf * 128 + c * (C::VKEYS / 2);
+                    // (both row tiles read a block: the first waits for its slots, the last gives them back)
+                    const bool first = t == 0, last = t == nt - 1;
+                    const int buf = C::TILES == 2 ? t : j & 1;
+                    if (j >= 0) {                       // O += P(j) V(j)
+                        if (ok) ok = mbar_wait(p_full(buf), (p_phase >> buf) & 1, abort_flag);
+                        p_phase ^= 1u << buf;
+                        Ring r = first ? ring : v_ring;
+                        if (first) v_ring = ring;
 #pragma unroll
-                                    for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-                                        umma_bf16_ts(tmem + C::O_COL + t * D, pa + ks * 8, vd + ks * (2048 >> 4), idesc_o, (j | c | ks) ? 1u : 0u);
-                                    if (last) umma_commit(empty(r.slot));
-                                }
-                                r.next(NS);
-                            }
-                            if (first) ring = r;
-                            if (ok) umma_commit(o_done(t));
-                        }
-                        if (j + C::LEAD < count) {      // S(j + LEAD) = Q K^T, over the P just used
-                            Ring r = first ? ring : k_ring;
-                            if (first) k_ring = ring;
-#pragma unroll 1
-                            for (int c = 0; c < C::KC; ++c) {
-                                if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
-                                if (ok) {
-                                    tc_fence_after_sync();
-                                    const uint64_t qd = umma_desc_k_sw128(s_q + t * C::Q_TILE + c * 16384u), kd = umma_desc_k_sw128(s_ring + r.slot * kSlot);
+                        for (int c = 0; c < C::VC; ++c) {
+                            if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (ok) {
+                                tc_fence_after_sync();
+                                const uint64_t vd = v_desc + r.slot * (kSlot >> 4);
+                                const uint32_t pa = tmem + buf * 128 + c * (C::VKEYS / 2);
 #pragma unroll
-                                    for (int ks = 0; ks < 4; ++ks)
-                                        umma_bf16(tmem + buf * 128, qd + ks * 2, kd + ks * 2, idesc_s, (c | ks) ? 1u : 0u);
-                                    if (last) umma_commit(empty(r.slot));
-                                }
-                                r.next(NS);
+                                for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+                                    umma_bf16_ts_warp(leader, tmem + C::O_COL + t * D, pa + ks * 8, vd + ks * (2048 >> 4), idesc_o,
+                                                      c + ks > 0 ? 1u : (uint32_t)j);
+                                if (last) umma_commit_warp(leader, empty(r.slot));
                             }
-                            if (first) ring = r;
-                            if (ok) umma_commit(s_full(buf));
+                            r.next(NS);
                         }
+                        if (first) ring = r;
+                        if (ok) umma_commit_warp(leader, o_done(t));
                     }
-            }
-            if (!ok) {                                  // MMAs in flight end before the tensor memory goes back
-                umma_commit(drained);
-                mbar_drain(drained, 0);
-            }
+                    if (j + C::LEAD < count) {          // S(j + LEAD) = Q K^T, over the P just used
+                        Ring r = first ? ring : k_ring;
+                        if (first) k_ring = ring;
+#pragma unroll
+                        for (int c = 0; c < C::KC; ++c) {
+                            if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (ok) {
+                                tc_fence_after_sync();
+                                const uint64_t qd = q_desc + (t * C::Q_TILE + c * 16384u) / 16, kd = k_desc + r.slot * (kSlot >> 4);
+#pragma unroll
+                                for (int ks = 0; ks < 4; ++ks)
+                                    umma_bf16_warp(leader, tmem + buf * 128, qd + ks * 2, kd + ks * 2, idesc_s, c + ks > 0 ? 1u : 0u);
+                                if (last) umma_commit_warp(leader, empty(r.slot));
+                            }
+                            r.next(NS);
+                        }
+                        if (first) ring = r;
+                        if (ok) umma_commit_warp(leader, s_full(buf));
+                    }
+                }
+        }
+        if (!ok) {                                      // MMAs in flight end before the tensor memory goes back
+            umma_commit_warp(leader, drained);
+            mbar_drain(drained, 0);
         }
         __syncwarp();
     }
