@@ -147,7 +147,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         while (next_item(a, walk, 16, C::BK, it)) {
             const ListInfo& li = it.li;
             const int tile = it.tile, b0 = it.b0;
-            const int head0 = (it.list % a.Hkv) * a.G;
+            const int head0 = (it.list - quotient(it.list, a.div_hkv) * a.Hkv) * a.G;
             // rows g8 and g8 + 8 of the tile
             int tok[2], hd[2], lim[2];
             bool live[2];
@@ -155,8 +155,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const int pr = tile * 16 + g8 + 8 * x;
-                tok[x] = pr / a.G;
-                hd[x] = head0 + pr % a.G;
+                tok[x] = quotient(pr, a.div_g);
+                hd[x] = head0 + pr - tok[x] * a.G;
                 live[x] = tok[x] < li.rows_tok;
                 lim[x] = live[x] ? limit_of(li, a, tok[x]) : 0;
                 const __nv_bfloat16* src = a.q + (long long)(li.q0 + (live[x] ? tok[x] : 0)) * a.q_stride + (long long)hd[x] * D;
@@ -305,11 +305,11 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                         for (int i = 0; i < D / 8; ++i) dst[i * 4] = pack_bf16(o[i][2 * x] * inv, o[i][2 * x + 1] * inv);
                         if (a.lse && t4 == 0) a.lse[row] = lse_of(mx[x], sum[x]);
                     } else {
-                        const size_t row = slot * 16 + g8 + 8 * x;
-                        float2* dst = reinterpret_cast<float2*>(a.part_o + row * D) + t4;
+                        // (parts: [D / 4][16 rows][4 channels])
+                        float2* dst = reinterpret_cast<float2*>(a.part_o + slot * 16 * D + ((t4 / 2) * 16 + g8 + 8 * x) * 4 + (t4 & 1) * 2);
 #pragma unroll
-                        for (int i = 0; i < D / 8; ++i) dst[i * 4] = make_float2(o[i][2 * x], o[i][2 * x + 1]);
-                        if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + row * 2) = make_float2(mx[x], sum[x]);
+                        for (int i = 0; i < D / 8; ++i) dst[i * 64] = make_float2(o[i][2 * x], o[i][2 * x + 1]);
+                        if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + g8 + 8 * x) * 2) = make_float2(mx[x], sum[x]);
                     }
                 }
             }
@@ -329,9 +329,10 @@ __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, in
     const int r = blockIdx.y, tile = blockIdx.x / GROUPS, row0 = blockIdx.x % GROUPS * 16;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const ListInfo li = list_info(a, r, false);
-    const long long rows_left = (long long)li.rows_tok * a.G - ((long long)tile * ROWS + row0);
+    const int head0 = (r - quotient(r, a.div_hkv) * a.Hkv) * a.G;
+    const int rows_left = li.rows_tok * a.G - (tile * ROWS + row0);
     if (rows_left <= 0) return;
-    const int live = rows_left < 16 ? (int)rows_left : 16;
+    const int live = min(rows_left, 16);
     long long before, total;
     count_units<128>(a, BK, ROWS, r, &before, &total);
     long long u0 = before;
@@ -363,15 +364,18 @@ __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, in
         const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
         for (int p = lane; p < parts; p += 32) weight[row][p] *= inv;
         if (lane == 0 && a.lse) {
-            const long long pr = (long long)tile * ROWS + row0 + row;
-            a.lse[(size_t)(li.q0 + (int)(pr / a.G)) * a.Hq + (r % a.Hkv) * a.G + (int)(pr % a.G)] = lse_of(m, l);
+            const int pr = tile * ROWS + row0 + row, tok = quotient(pr, a.div_g);
+            a.lse[(size_t)(li.q0 + tok) * a.Hq + head0 + pr - tok * a.G] = lse_of(m, l);
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < live * (D / 4); i += 128) {
-        const int row = i / (D / 4), col = i % (D / 4) * 4;
-        const float* src = a.part_o + (p0 + row) * D + col;
-        const float* next = a.part_o + (p1 + row) * D + col;
+    // (a part's rows lie side by side in pieces of 4 channels: [D / 4][ROWS][4])
+    const int bits = live > 8 ? 4 : live > 4 ? 3 : live > 2 ? 2 : live - 1;
+    for (int i = threadIdx.x; i < (D / 4) << bits; i += 128) {
+        const int row = i & ((1 << bits) - 1), col = (i >> bits) * 4;
+        if (row >= live) continue;
+        const float* src = a.part_o + (p0 - row0) * D + (size_t)(col * ROWS) + (row0 + row) * 4;
+        const float* next = a.part_o + (p1 - row0) * D + (size_t)(col * ROWS) + (row0 + row) * 4;
         float4 o = *reinterpret_cast<const float4*>(src);
         const float w0 = weight[row][0];
         o = make_float4(o.x * w0, o.y * w0, o.z * w0, o.w * w0);
@@ -384,8 +388,8 @@ __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, in
             o.z += v.z * w;
             o.w += v.w * w;
         }
-        const long long pr = (long long)tile * ROWS + row0 + row;
-        const size_t at = (size_t)(li.q0 + (int)(pr / a.G)) * a.Hq + (r % a.Hkv) * a.G + (int)(pr % a.G);
+        const int pr = tile * ROWS + row0 + row, tok = quotient(pr, a.div_g);
+        const size_t at = (size_t)(li.q0 + tok) * a.Hq + head0 + pr - tok * a.G;
         *reinterpret_cast<uint2*>(a.out + at * D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
     }
 }
@@ -482,6 +486,8 @@ extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape
     a.n_tokens = n_tokens;
     a.max_q = max_q;
     a.causal = causal != 0;
+    a.div_g = fast_div(a.G);
+    a.div_hkv = fast_div(a.Hkv);
     a.scale_log2 = scale * 1.4426950408889634f;
     int prev = 0;
     EA_CUDA_TRY(cudaGetDevice(&prev));

@@ -6,6 +6,19 @@
 
 #include "ea_internal.h"
 
+// Division of 0 <= n < 2^31 by a fixed d >= 1 without a divide: with l = ceil(log2 d) and mul = ceil(2^(31 + l) / d) < 2^32,
+// mul d exceeds 2^(31 + l) by less than 2^l, so that n mul / 2^(31 + l) is off by less than 1 / d.
+struct FastDiv {
+    uint32_t mul;
+    int shift, d;
+};
+static inline FastDiv fast_div(int d) {
+    int l = 0;
+    while ((1 << l) < d) ++l;
+    return {d == 1 ? 0u : (uint32_t)(((1ull << (31 + l)) + (uint32_t)d - 1) / (uint32_t)d), l - 1, d};
+}
+__device__ __forceinline__ int quotient(int n, const FastDiv& f) { return f.shift < 0 ? n : (int)(__umulhi((uint32_t)n, f.mul) >> f.shift); }
+
 struct AttnArgs {
     const __nv_bfloat16* q;
     long long q_stride;          // elements between tokens
@@ -18,6 +31,7 @@ struct AttnArgs {
     float* part_ml;              // their maxima (of scores in units of log 2) and sums
     int* status;
     int lists, Hq, Hkv, G, shift, n_pages, max_pages, n_tokens, max_q, causal;
+    FastDiv div_g, div_hkv;      // by G and by Hkv
     float scale_log2;
 };
 
@@ -30,7 +44,7 @@ struct ListInfo {
 
 // Lengths and offsets live on the device, so they are checked here: what does not fit is reported and left out.
 __device__ __forceinline__ ListInfo list_info(const AttnArgs& a, int r, bool report) {
-    const int s = r / a.Hkv;
+    const int s = quotient(r, a.div_hkv);
     const int q0 = a.q_off[s], q1 = a.q_off[s + 1];
     ListInfo li = {0, 0, 0, 0};
     bool bad = q0 < 0 || q1 < q0 || q1 > a.n_tokens;
@@ -50,19 +64,18 @@ __device__ __forceinline__ ListInfo list_info(const AttnArgs& a, int r, bool rep
     if (bad && report) a.status[1] = (int)EA_ERR_PAGES;
     return li;
 }
-__device__ __forceinline__ int tiles_of(const ListInfo& li, const AttnArgs& a, int rows) {
-    return (int)(((long long)li.rows_tok * a.G + rows - 1) / rows);
-}
+// (packed rows of a call are below 2^31: n_tokens * Hq is)
+__device__ __forceinline__ int tiles_of(const ListInfo& li, const AttnArgs& a, int rows) { return (int)(((unsigned)(li.rows_tok * a.G) + rows - 1u) / (unsigned)rows); }
 // First row of a list that token `tok` does not see.
 __device__ __forceinline__ int limit_of(const ListInfo& li, const AttnArgs& a, int tok) {
     if (!a.causal) return li.n;
-    const long long v = (long long)li.n - li.m + tok + 1;
-    return v < 0 ? 0 : v < li.n ? (int)v : li.n;
+    const int v = li.n - li.m + tok + 1;                 // tok < m: between -2^31 and n
+    return v < 0 ? 0 : v;
 }
 // Key blocks that a row tile looks at: one at least, so that rows which see nothing still have their outputs written.
 __device__ __forceinline__ int tile_blocks(const ListInfo& li, const AttnArgs& a, int tile, int rows, int BK) {
-    const long long last = (((long long)tile + 1) * rows - 1) / a.G;
-    const int lim = limit_of(li, a, last < li.rows_tok ? (int)last : li.rows_tok - 1);
+    const int end = min((tile + 1) * rows, li.rows_tok * a.G);
+    const int lim = limit_of(li, a, quotient(end - 1, a.div_g));
     return lim > BK ? (int)(((unsigned)lim + BK - 1u) / BK) : 1;
 }
 __device__ __forceinline__ long long list_units(const ListInfo& li, const AttnArgs& a, int rows, int BK) {

@@ -33,12 +33,13 @@ template <int D> struct Chunk {
     static constexpr int VC = kBK / VKEYS;
     static constexpr int PER_BLOCK = KC + VC;
     static constexpr uint32_t Q_TILE = 128u * D * 2;
-    static constexpr int NSLOT = D == 64 ? 12 : 10;
-    static constexpr int THREADS = 128 + TILES * 128;   // warps 0 (loads), 1 (MMA), two idle, then the softmax warps
-    // registers: 384 threads x 168 = 128 x 80 + 256 x 208 at most; 256 threads start with enough for everyone
+    static constexpr int NSLOT = D == 64 ? 11 : 9;
+    static constexpr int THREADS = 128 + TILES * 256;   // warps 0 (loads), 1 (MMA), two idle, then the softmax warps
+    // registers: 640 threads x 96 = 128 x 64 + 512 x 104; 384 threads start with enough for everyone
     static constexpr bool SPLIT = TILES == 2;
-    static constexpr int BARS = 2 * NSLOT + 9;
-    static constexpr int TAIL = BARS * 8 + 16 + (int)sizeof(Walk);
+    static constexpr int BARS = 2 * NSLOT + 11;
+    static constexpr int TAIL_STATS = BARS * 8 + 16 + (int)sizeof(Walk);
+    static constexpr int TAIL = TAIL_STATS + TILES * 2 * 2 * 128 * 4;       // [tile][parity of the block][half][row]
     static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)kSlot + TAIL;
     static constexpr uint32_t O_COL = 256;              // tensor memory: S (P) at 0 and 128, O from 256
     static_assert(SMEM + 1024 <= 232448, "a CTA's shared memory, with room for static arrays");
@@ -60,6 +61,35 @@ struct Ring {
     }
 };
 
+// 2^(c s - z) on the FMA pipe, two scores at a time, for whole z with |z| < 2^20 and scores that are not masked: adding
+// K = 1.5 * 2^23 + 127 - z rounds c s to a whole number n (Cody and Waite's reduction), which leaves the exponent field
+// of 2^(n - z) in the low bits and f = c s - n in [-1/2, 1/2]; 2^f by the minimax polynomial of degree 5 (Remez exchange
+// on the relative error: 7.5e-8, 2.1e-7 as evaluated in fp32, the size of ex2.approx's own).  Scores 126 below z stop
+// there.  A NaN stays one.  ex2 takes 8 issue cycles of a scheduler per warp, 16 for the pair, this 18 of another pipe:
+// three pairs of eight this way balance the two (the pipes also carry the sums and conversions).
+#ifndef POLY
+#define POLY(i) false
+#endif
+struct Exp2Poly {
+    float2 c, K;
+    float lo;
+    __device__ __forceinline__ Exp2Poly(float scale, float inv_scale, float z)
+        : c(make_float2(scale, scale)), K(make_float2(12583039.f - z, 12583039.f - z)), lo((z - 126.f) * inv_scale) {}
+    static __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+    __device__ __forceinline__ float2 operator()(float2 s) const {
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(s.x) : "f"(lo));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(s.y) : "f"(lo));
+        const float2 t = fma2(s, c, K);
+        const float2 f = fma2(s, c, fma2(t, both(-1.f), K));
+        float2 p = fma2(both(0.0013276472454890609f), f, both(0.009675540961325169f));
+        p = fma2(p, f, both(0.05550713092088699f));
+        p = fma2(p, f, both(0.24022120237350464f));
+        p = fma2(p, f, both(0.6931469440460205f));
+        p = fma2(p, f, both(1.0000001192092896f));
+        return mul2(p, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
+    }
+};
+
 template <int D>
 __global__ void __launch_bounds__(Chunk<D>::THREADS, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
@@ -78,7 +108,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     auto p_full = [&](int t) { return bars + 8u * (2 * NS + 2 + t); };
     auto o_done = [&](int t) { return bars + 8u * (2 * NS + 4 + t); };
     auto q_full = [&](int t) { return bars + 8u * (2 * NS + 6 + t); };
-    const uint32_t drained = bars + 8u * (2 * NS + 8);  // only used when a wait has given up
+    auto p_rest = [&](int t) { return bars + 8u * (2 * NS + 8 + t); };
+    const uint32_t drained = bars + 8u * (2 * NS + 10);  // only used when a wait has given up
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * C::BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
     Walk* start = reinterpret_cast<Walk*>(tail + 8 * C::BARS + 16);
@@ -91,9 +122,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(s_full(t), 1);
-            mbar_init(p_full(t), 4);
+            mbar_init(p_full(t), 4);                    // weights of the block's first 64 keys; p_rest: of the others
+            mbar_init(p_rest(t), 4);
             mbar_init(o_done(t), 1);
-            mbar_init(q_full(t), 4);
+            mbar_init(q_full(t), 8);
         }
         mbar_init(drained, 1);
         *abort_flag = 0;
@@ -109,13 +141,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     Walk walk = *start;
     Item it;
     bool ok = true;
 
     if (warp < 4) {
-    if (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0) {
         // ------------------------------------------------------------------------------ K and V
         Ring ring = {0, 0};
@@ -194,7 +226,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         Ring ring = {0, 0}, k_ring = {0, 0}, v_ring = {0, 0};
         while (next_item(a, walk, C::ROWS, kBK, it)) {
             const int count = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
-            const long long rows = (long long)it.li.rows_tok * a.G - (long long)it.tile * C::ROWS;
+            const int rows = it.li.rows_tok * a.G - it.tile * C::ROWS;
             const int nt = __shfl_sync(0xffffffffu, C::TILES == 2 && rows > 128 ? 2 : 1, 0);
             for (int t = 0; t < nt; ++t) {
                 if (ok) ok = mbar_wait(q_full(t), (q_phase >> t) & 1, abort_flag);
@@ -209,7 +241,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     const int buf = C::TILES == 2 ? t : j & 1;
                     if (j >= 0) {                       // O += P(j) V(j)
                         if (ok) ok = mbar_wait(p_full(buf), (p_phase >> buf) & 1, abort_flag);
-                        p_phase ^= 1u << buf;
                         Ring r = first ? ring : v_ring;
                         if (first) v_ring = ring;
 #pragma unroll
@@ -221,13 +252,19 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                                 const uint64_t vd = v_desc + r.slot * (kSlot >> 4);
                                 const uint32_t pa = tmem + buf * 128 + c * (C::VKEYS / 2);
 #pragma unroll
-                                for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+                                for (int ks = 0; ks < C::VKEYS / 16; ++ks) {
+                                    if (c * C::VKEYS + ks * 16 == kBK / 2) {
+                                        ok = __all_sync(0xffffffffu, mbar_wait(p_rest(buf), (p_phase >> buf) & 1, abort_flag));
+                                        tc_fence_after_sync();
+                                    }
                                     umma_bf16_ts_warp(leader, tmem + C::O_COL + t * D, pa + ks * 8, vd + ks * (2048 >> 4), idesc_o,
                                                       c + ks > 0 ? 1u : (uint32_t)j);
+                                }
                                 if (last) umma_commit_warp(leader, empty(r.slot));
                             }
                             r.next(NS);
                         }
+                        p_phase ^= 1u << buf;
                         if (first) ring = r;
                         if (ok) umma_commit_warp(leader, o_done(t));
                     }
@@ -260,59 +297,79 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         __syncwarp();
     }
     } else {
-        if (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        // ------------------------------------------------------------------------------ softmax, one row per thread
-        const int t = (warp - 4) / 4, quarter = warp & 3;
+        if (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        // ------------------------------------------------------------------------------ softmax, two threads per row
+        // Warps w and w + 4 of a row tile share its 32 rows: one takes keys 0-63 of a block, the other 64-127 (half the
+        // chain of instructions between scores and weights, and four warps per scheduler to fill the pipes).  They agree
+        // on the maximum through shared memory.
+        const int t = (warp - 4) / 8, half = ((warp - 4) >> 2) & 1, quarter = warp & 3;
         const int row = quarter * 32 + lane;            // tensor-memory lanes follow warp % 4
+        const int pair = 1 + t * 4 + quarter;           // named barrier of the two warps
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const uint32_t o_col = tmem + lanes + C::O_COL + t * D;
-        uint32_t n_s[2] = {0, 0}, n_o = 0;
+        const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * (D / 2);
+        float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS) + t * 512;
+        uint32_t n_s[2] = {0, 0}, n_o = 0, turn = 0;
         long long seq = 0;                              // ring slots of the items before this one
-        const float sign = a.scale_log2 < 0.f ? -1.f : 1.f;
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
         // any score but does not make NaN of a masked one (-infinity)
         const float scale = a.scale_log2 == 0.f ? 1e-37f : fabsf(a.scale_log2);
+        const float inv_scale = 1.f / scale;
+        // the partner's value of a pair of threads (both call it, `turn` alternates the buffers)
+        auto partner = [&](float mine) {
+            float* at = stats + (turn & 1) * 256;
+            at[half * 128 + row] = mine;
+            bar_sync(pair, 64);
+            ++turn;
+            return at[(half ^ 1) * 128 + row];
+        };
         while (next_item(a, walk, C::ROWS, kBK, it)) {
             const ListInfo& li = it.li;
             const int count = it.b1 - it.b0;
-            const long long live_rows = (long long)li.rows_tok * a.G - (long long)it.tile * C::ROWS;
+            const int live_rows = li.rows_tok * a.G - it.tile * C::ROWS;
             const int nt = C::TILES == 2 && live_rows > 128 ? 2 : 1;
             if (t >= nt) {
                 seq += (long long)count * C::PER_BLOCK;
                 continue;
             }
             // ---- queries: 16 bytes per thread and step, rows without a query are zero
-            const int head0 = (it.list % a.Hkv) * a.G;
-            const int tid = threadIdx.x - 128 - t * 128;
-            const long long row0 = (long long)it.tile * C::ROWS + t * 128;
-            constexpr int PIECES = D / 8;
-#pragma unroll 4
-            for (int i = tid; i < 128 * PIECES; i += 128) {
-                const int r = i / PIECES, piece = i % PIECES;
-                const long long pr = row0 + r;
-                const int tok = (int)(pr / a.G), h = head0 + (int)(pr % a.G);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (tok < li.rows_tok) {
-                    v = *reinterpret_cast<const uint4*>(a.q + (long long)(li.q0 + tok) * a.q_stride + (long long)h * D + piece * 8);
-                    if (sign < 0.f) {
-                        v.x ^= 0x80008000u;
-                        v.y ^= 0x80008000u;
-                        v.z ^= 0x80008000u;
-                        v.w ^= 0x80008000u;
-                    }
+            const int head0 = (it.list - quotient(it.list, a.div_hkv) * a.Hkv) * a.G;
+            const int row0 = it.tile * C::ROWS + t * 128, tid = threadIdx.x - 128 - t * 256;
+            constexpr int PIECES = D / 8, STEPS = 128 * PIECES / 256, BATCH = STEPS < 8 ? STEPS : 8;
+            // (the same thread that stored an output piece in this place, so the place is free)
+            const uint32_t q_tile = s_q + t * C::Q_TILE;
+            auto q_place = [&](int r, int piece) { return q_tile + (piece / 8) * 16384u + r * 128u + (((piece % 8) * 16u) ^ ((r & 7) * 16u)); };
+#pragma unroll
+            for (int i0 = 0; i0 < STEPS; i0 += BATCH) {
+                uint4 v[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int at = (i0 + i) * 256 + tid, r = at / PIECES, piece = at % PIECES;
+                    const int tok = quotient(row0 + r, a.div_g), h = head0 + row0 + r - tok * a.G;
+                    v[i] = make_uint4(0, 0, 0, 0);
+                    if (tok < li.rows_tok)
+                        v[i] = __ldg(reinterpret_cast<const uint4*>(a.q + (li.q0 + tok) * a.q_stride + (long long)h * D + piece * 8));
                 }
-                sts128(s_q + t * C::Q_TILE + (piece / 8) * 16384u + r * 128u + (((piece % 8) * 16u) ^ ((r & 7) * 16u)), v);
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int at = (i0 + i) * 256 + tid;
+                    if (a.scale_log2 < 0.f) {
+                        v[i].x ^= 0x80008000u;
+                        v[i].y ^= 0x80008000u;
+                        v[i].z ^= 0x80008000u;
+                        v[i].w ^= 0x80008000u;
+                    }
+                    sts128(q_place(at / PIECES, at % PIECES), v[i]);
+                }
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full(t));
 
-            const long long pr = row0 + row;
-            const int tok = (int)(pr / a.G), head = head0 + (int)(pr % a.G);
+            const int tok = quotient(row0 + row, a.div_g);
             const bool live = tok < li.rows_tok;
             const int lim = live ? limit_of(li, a, tok) : 0;
             // keys that every row of the tile sees
-            const int seen = limit_of(li, a, (int)(row0 / a.G));
+            const int seen = limit_of(li, a, quotient(row0, a.div_g));
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < count; ++j) {
                 const int key0 = (it.b0 + j) * kBK;
@@ -322,18 +379,18 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 ok = __all_sync(0xffffffffu, ok);
                 if (key0 + kBK > li.n && t == 0) {
                     // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN:
-                    // they become zero before the product is let go.  (A parity tells two neighbouring phases apart: with
+                    // each half makes its own zero before its weights let the product go.  (A parity tells two neighbouring phases apart: with
                     // scores a block ahead, the slots' earlier use is only known to be over when the product before is.)
                     if (C::TILES == 1 && j > 0 && ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
                     for (int c = 0; c < C::VC; ++c) {
                         const long long at = seq + C::v_at(j, count) + c;
                         const uint32_t s = (uint32_t)(at % NS);
-                        const int from = max(0, li.n - key0 - c * C::VKEYS);
-                        if (from >= C::VKEYS) continue;
+                        const int from = max(half * 64, li.n - key0) - c * C::VKEYS, to = half * 64 + 64 - c * C::VKEYS;
+                        const int r0 = max(from, 0), r1 = min(to, C::VKEYS);
+                        if (r0 >= r1) continue;
                         if (ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
-                        const int todo = (C::VKEYS - from) * PIECES;
-                        for (int i = tid; i < todo; i += 128) {
-                            const int r = from + i / PIECES, piece = i % PIECES;
+                        for (int i = tid & 127; i < (r1 - r0) * PIECES; i += 128) {
+                            const int r = r0 + i / PIECES, piece = i % PIECES;
                             sts128(s_ring + s * kSlot + (piece / 8) * (C::VKEYS * 128u) + r * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
                         }
                     }
@@ -342,33 +399,38 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 __syncwarp();
                 tc_fence_after_sync();
                 const uint32_t s_col = tmem + lanes + buf * 128;
-                uint32_t x[4][32];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld_x32(s_col + i * 32, x[i]);
+                uint32_t x[2][32];
+                tmem_ld_x32(s_col + half * 64, x[0]);
+                tmem_ld_x32(s_col + half * 64 + 32, x[1]);
                 tmem_ld_wait();
                 if (key0 + kBK > seen) {
-                    const int local = lim - key0;
+                    const int local = lim - key0 - half * 64;
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
+                    for (int i = 0; i < 64; ++i)
                         if (i >= local) x[i / 32][i % 32] = 0xff800000u;
                 }
                 float top[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    top[i] = __uint_as_float(x[i][0]);
+                    top[i] = __uint_as_float(x[i / 2][i % 2 * 16]);
 #pragma unroll
-                    for (int e = 1; e < 31; e += 2) top[i] = max3(top[i], __uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1]));
-                    top[i] = fmaxf(top[i], __uint_as_float(x[i][31]));
+                    for (int e = 1; e < 15; e += 2)
+                        top[i] = max3(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + e]), __uint_as_float(x[i / 2][i % 2 * 16 + e + 1]));
+                    top[i] = fmaxf(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + 15]));
                 }
-                const float m_blk = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+                tc_fence_before_sync();                 // the partner's weights go over scores read here
+                const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                const float m_blk = fmaxf(mine, partner(mine)) * scale;
+                tc_fence_after_sync();
                 bool move = false;
                 float f = 1.f;
                 if (m == -INFINITY) {
-                    m = m_blk;                          // nothing seen so far: sum and output are zero
+                    m = ceilf(m_blk);                   // nothing seen so far: sum and output are zero
                 } else if (m_blk > m + kRescale) {
-                    f = ex2(m - m_blk);
+                    const float up = ceilf(m_blk);
+                    f = ex2(m - up);
                     l *= f;
-                    m = m_blk;
+                    m = up;
                     move = true;
                 }
                 if (__any_sync(0xffffffffu, move)) {
@@ -377,38 +439,62 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     ok = __all_sync(0xffffffffu, ok);
                     tc_fence_after_sync();
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld_x32(o_col + c, o);
+                    for (int c = 0; c < D / 2; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld_x16(o_col + c, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st_x32(o_col + c, o);
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st_x16(o_col + c, o);
                     }
                 }
                 const float z = m == -INFINITY ? 0.f : m;
                 const float2 c2 = make_float2(scale, scale), z2 = make_float2(-z, -z);
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                // the polynomial's range reduction wants small whole z and no masked score
+                if (__all_sync(0xffffffffu, key0 + kBK <= seen && fabsf(z) < 1048576.f)) {
+                    const Exp2Poly e2(scale, inv_scale, z);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t p[16];
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t p[16];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
-                        y.x = ex2(y.x);
-                        y.y = ex2(y.y);
-                        sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
-                        p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
+                        for (int e = 0; e < 32; e += 2) {
+                            float2 y = make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1]));
+                            if (POLY(e / 2)) {
+                                y = e2(y);
+                            } else {
+                                y = fma2(y, c2, z2);
+                                y.x = ex2(y.x);
+                                y.y = ex2(y.y);
+                            }
+                            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
+                            p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
+                        }
+                        tmem_st_x16(s_col + half * 32 + i * 16, p);
                     }
-                    tmem_st_x16(s_col + i * 16, p);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
+                            y.x = ex2(y.x);
+                            y.y = ex2(y.y);
+                            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
+                            p[e / 2] = pack_bf16(y.x, y.y);
+                        }
+                        tmem_st_x16(s_col + half * 32 + i * 16, p);
+                    }
                 }
-                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(buf));
+                if (lane == 0) mbar_arrive(half == 0 ? p_full(buf) : p_rest(buf));
+                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
-            // ---- output
+            // ---- output: each half its channels
+            l += partner(l);
             n_o += (uint32_t)count;
             // (a parity tells two neighbouring phases apart.  With scores a block ahead, all that is known here is that
             // the product of two blocks before the last has ended, so its successor is waited for on its own)
@@ -418,14 +504,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             tc_fence_after_sync();
             const bool whole = it.b0 == 0 && it.b1 == it.blocks;
             const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-            const size_t at = (size_t)(li.q0 + tok) * a.Hq + head;
-            const size_t part = ((size_t)2 * blockIdx.x + (it.first ? 0 : 1)) * C::ROWS + t * 128 + row;
+            if (whole) {
+                // through shared memory (where the queries were: every product with them has ended), so that rows leave
+                // in one piece
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                tmem_ld_x32(o_col + c, o);
-                tmem_ld_wait();
-                if (live && whole) {
+                for (int c = 0; c < D / 2; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld_x32(o_col + c, o);
+                    tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         uint4 v;
@@ -433,23 +519,36 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
                         v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
                         v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                        *reinterpret_cast<uint4*>(a.out + at * D + c + e) = v;
+                        sts128(q_place(row, (half * (D / 2) + c + e) / 8), v);
                     }
-                } else if (live) {
+                }
+                bar_sync(9 + t, 256);
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    const int at = i * 256 + tid, r = at / PIECES, piece = at % PIECES;
+                    const int tk = quotient(row0 + r, a.div_g), h = head0 + row0 + r - tk * a.G;
+                    if (tk < li.rows_tok)
+                        *reinterpret_cast<uint4*>(a.out + ((size_t)(li.q0 + tk) * a.Hq + h) * D + piece * 8) = lds128(q_place(r, piece));
+                }
+                if (live && half == 0 && a.lse) a.lse[(size_t)(li.q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G] = lse_of(m, l);
+            } else {
+                // a part: [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) write side by side
+                const size_t slot = (size_t)2 * blockIdx.x + (it.first ? 0 : 1);
+                float* dst = a.part_o + slot * C::ROWS * D + (t * 128 + row) * 4;
+#pragma unroll 1
+                for (int c = 0; c < D / 2; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld_x32(o_col + c, o);
+                    tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4*>(a.part_o + part * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        *reinterpret_cast<uint4*>(dst + (half * (D / 2) + c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 }
-                __syncwarp();
+                if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * C::ROWS + t * 128 + row) * 2) = make_float2(m, l);
             }
-            if (live) {
-                if (whole) {
-                    if (a.lse) a.lse[at] = lse_of(m, l);
-                } else {
-                    *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(m, l);
-                }
-            }
-            // (the loads above precede this warp's next arrival, which lets the next item's product overwrite O)
+            __syncwarp();
+            // (the loads above precede this pair's next exchange, and with it the weights that let the next item's
+            // product overwrite O)
             tc_fence_before_sync();
             seq += (long long)count * C::PER_BLOCK;
         }
