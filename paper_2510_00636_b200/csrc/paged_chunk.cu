@@ -1,13 +1,13 @@
 // Attention of chunks of new tokens over the paged cache on the tensor cores (tcgen05).
 //
 // A CTA works on row tiles of 128 packed rows (row = token * G + head), two of them at head_dim <= 128, one at 256 (the
-// output of a tile takes head_dim of the 512 tensor-memory columns, its scores 128), against blocks of 128 keys:
-//     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
-//     P = 2^(c S - m)  one thread per row: running maximum m, sum l; P (bf16) over S in tensor memory
+// output of a tile takes head_dim of the 512 tensor-memory columns), against blocks of 64 (two tiles) or 128 keys:
+//     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory, two buffers per tile
+//     P = 2^(c S - m)  running maximum m and sum l per row; P (bf16) over S in tensor memory
 //     O += P V         A = P from tensor memory, B = V as it lies (rows are the contraction index: MN-major)
-// One warp keeps K and V flowing through a ring of 16 KiB slots (TMA boxes of a page each), one thread issues the MMAs,
-// and four warps per row tile do the softmax.  With two row tiles the tensor cores work on one while the softmax works on
-// the other; with one, on the scores of the next block.
+// One warp keeps K and V flowing through a ring of slots (TMA boxes of a page each), one warp per row tile issues its MMAs
+// (the waits of one are hidden by the other's), eight warps do the softmax, 64 scores per thread and block.  The scores of
+// the next block are there when the softmax of one ends.
 //
 // The running maximum only moves when a row's scores exceed it by more than 2^8 (the weights then stay within fp32 and
 // bf16 range, and the sum, which uses the same maximum, cancels it): O is rescaled in tensor memory only then.
@@ -21,33 +21,32 @@ using namespace ptx;
 
 namespace {
 
-constexpr int kBK = 128;                                // keys per block
-constexpr uint32_t kSlot = 16384;
 constexpr float kRescale = 8.0f;
+constexpr int kLead = 2;                                // blocks that the scores run ahead of the product
 
 template <int D> struct Chunk {
     static constexpr int TILES = D == 256 ? 1 : 2;
+    static constexpr int HALVES = 2 / TILES;            // threads per row (each has 64 keys of a block)
     static constexpr int ROWS = TILES * 128;
-    static constexpr int KC = D / 64;                   // slots of a K block: 128 keys x 64 channels each
-    static constexpr int VKEYS = 8192 / D;              // keys of a V slot: all channels
-    static constexpr int VC = kBK / VKEYS;
+    static constexpr int BK = HALVES * 64;              // keys per block
+    // a slot of the ring: K: all keys of a block x KW * 64 channels;  V: VKEYS keys x all channels
+    static constexpr uint32_t SLOT = D == 64 ? 8192 : 16384;
+    static constexpr int KW = (int)SLOT / (BK * 128), KC = D / 64 / KW;
+    static constexpr int VKEYS = (int)SLOT / (D * 2), VC = BK / VKEYS;
     static constexpr int PER_BLOCK = KC + VC;
     static constexpr uint32_t Q_TILE = 128u * D * 2;
-    static constexpr int NSLOT = D == 64 ? 11 : 9;
-    static constexpr int THREADS = 128 + TILES * 256;   // warps 0 (loads), 1 (MMA), two idle, then the softmax warps
-    // registers: 640 threads x 96 = 128 x 64 + 512 x 104; 384 threads start with enough for everyone
-    static constexpr bool SPLIT = TILES == 2;
-    static constexpr int BARS = 2 * NSLOT + 11;
-    static constexpr int TAIL_STATS = BARS * 8 + 16 + (int)sizeof(Walk);
-    static constexpr int TAIL = TAIL_STATS + TILES * 2 * 2 * 128 * 4;       // [tile][parity of the block][half][row]
-    static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)kSlot + TAIL;
-    static constexpr uint32_t O_COL = 256;              // tensor memory: S (P) at 0 and 128, O from 256
-    static_assert(SMEM + 1024 <= 232448, "a CTA's shared memory, with room for static arrays");
-    // Scores run LEAD blocks ahead of the product.  Order of the blocks in the ring: with two row tiles K0 V0 K1 V1 ...,
-    // with one K0 K1 V0 K2 V1 ...
-    static constexpr int LEAD = TILES == 2 ? 1 : 2;
-    // where block j's V begins, in slots after the item's first
-    static __device__ __forceinline__ int v_at(int j, int count) { return (j + LEAD < count ? j + LEAD : count) * KC + j * VC; }
+    static constexpr int NSLOT = D == 64 ? 20 : D == 128 ? 10 : 9;
+    static constexpr int THREADS = 128 + 256;           // warps 0 (loads), 1 and 2 (MMA of a row tile), an idle one, the softmax warps
+    static constexpr int BARS = 2 * NSLOT + 14;
+    static constexpr int TAIL_WALK = BARS * 8 + 16;
+    static constexpr int TAIL_STATS = TAIL_WALK + (int)sizeof(Walk);
+    static constexpr int TAIL = TAIL_STATS + (HALVES == 2 ? 2 * 2 * 128 * 4 : 0);      // [turn][half][row]
+    static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)SLOT + TAIL;
+    static constexpr uint32_t O_COL = 256;              // tensor memory: S (P) of tile t, buffer b at (2 t + b) BK, O from 256
+    static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
+    static_assert(KC * KW * 64 == D && VC * VKEYS == BK && VKEYS % 16 == 0, "slots");
+    // Order of the blocks in the ring: K0 K1 V0 K2 V1 ...; where block j's V begins, in slots after the item's first
+    static __device__ __forceinline__ int v_at(int j, int count) { return (j + kLead < count ? j + kLead : count) * KC + j * VC; }
 };
 
 // A place in the ring: slot, and the parity of its use.
@@ -61,73 +60,44 @@ struct Ring {
     }
 };
 
-// 2^(c s - z) on the FMA pipe, two scores at a time, for whole z with |z| < 2^20 and scores that are not masked: adding
-// K = 1.5 * 2^23 + 127 - z rounds c s to a whole number n (Cody and Waite's reduction), which leaves the exponent field
-// of 2^(n - z) in the low bits and f = c s - n in [-1/2, 1/2]; 2^f by the minimax polynomial of degree 5 (Remez exchange
-// on the relative error: 7.5e-8, 2.1e-7 as evaluated in fp32, the size of ex2.approx's own).  Scores 126 below z stop
-// there.  A NaN stays one.  ex2 takes 8 issue cycles of a scheduler per warp, 16 for the pair, this 18 of another pipe:
-// three pairs of eight this way balance the two (the pipes also carry the sums and conversions).
-#ifndef POLY
-#define POLY(i) false
-#endif
-struct Exp2Poly {
-    float2 c, K;
-    float lo;
-    __device__ __forceinline__ Exp2Poly(float scale, float inv_scale, float z)
-        : c(make_float2(scale, scale)), K(make_float2(12583039.f - z, 12583039.f - z)), lo((z - 126.f) * inv_scale) {}
-    static __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-    __device__ __forceinline__ float2 operator()(float2 s) const {
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(s.x) : "f"(lo));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(s.y) : "f"(lo));
-        const float2 t = fma2(s, c, K);
-        const float2 f = fma2(s, c, fma2(t, both(-1.f), K));
-        float2 p = fma2(both(0.0013276472454890609f), f, both(0.009675540961325169f));
-        p = fma2(p, f, both(0.05550713092088699f));
-        p = fma2(p, f, both(0.24022120237350464f));
-        p = fma2(p, f, both(0.6931469440460205f));
-        p = fma2(p, f, both(1.0000001192092896f));
-        return mul2(p, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
-    }
-};
-
 template <int D>
 __global__ void __launch_bounds__(Chunk<D>::THREADS, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const AttnArgs a) {
     using C = Chunk<D>;
-    constexpr int NS = C::NSLOT;
+    constexpr int NS = C::NSLOT, BK = C::BK;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t s_q = base, s_ring = base + C::TILES * C::Q_TILE;
-    const uint32_t bars = s_ring + NS * kSlot;
-    uint8_t* tail = gen + C::TILES * C::Q_TILE + NS * kSlot;
+    const uint32_t bars = s_ring + NS * C::SLOT;
+    uint8_t* tail = gen + C::TILES * C::Q_TILE + NS * C::SLOT;
     auto full = [&](uint32_t s) { return bars + 8u * s; };
     auto empty = [&](uint32_t s) { return bars + 8u * (NS + s); };
-    // per row tile (S and P: per score buffer)
-    auto s_full = [&](int t) { return bars + 8u * (2 * NS + t); };
-    auto p_full = [&](int t) { return bars + 8u * (2 * NS + 2 + t); };
-    auto o_done = [&](int t) { return bars + 8u * (2 * NS + 4 + t); };
-    auto q_full = [&](int t) { return bars + 8u * (2 * NS + 6 + t); };
-    auto p_rest = [&](int t) { return bars + 8u * (2 * NS + 8 + t); };
-    const uint32_t drained = bars + 8u * (2 * NS + 10);  // only used when a wait has given up
+    // per row tile t and score buffer b
+    auto s_full = [&](int t, int b) { return bars + 8u * (2 * NS + 2 * t + b); };
+    auto p_full = [&](int t, int b) { return bars + 8u * (2 * NS + 4 + 2 * t + b); };
+    auto o_done = [&](int t) { return bars + 8u * (2 * NS + 8 + t); };
+    auto q_full = [&](int t) { return bars + 8u * (2 * NS + 10 + t); };
+    auto drained = [&](int t) { return bars + 8u * (2 * NS + 12 + t); };      // only used when a wait has given up
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * C::BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
-    Walk* start = reinterpret_cast<Walk*>(tail + 8 * C::BARS + 16);
+    Walk* start = reinterpret_cast<Walk*>(tail + C::TAIL_WALK);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
             mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
+            mbar_init(empty(s), C::TILES);
         }
         for (int t = 0; t < 2; ++t) {
-            mbar_init(s_full(t), 1);
-            mbar_init(p_full(t), 4);                    // weights of the block's first 64 keys; p_rest: of the others
-            mbar_init(p_rest(t), 4);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(s_full(t, b), 1);
+                mbar_init(p_full(t, b), 4 * C::HALVES);
+            }
             mbar_init(o_done(t), 1);
-            mbar_init(q_full(t), 8);
+            mbar_init(q_full(t), 4 * C::HALVES);
+            mbar_init(drained(t), 1);
         }
-        mbar_init(drained, 1);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tensormap(&k_map);
@@ -137,7 +107,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
         tmem_relinquish();
     }
-    find_range<C::THREADS>(a, kBK, C::ROWS, blockIdx.x, gridDim.x, start);
+    find_range<C::THREADS>(a, BK, C::ROWS, blockIdx.x, gridDim.x, start);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -146,13 +116,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     Item it;
     bool ok = true;
 
-    if (warp < 4) {
-    if (C::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0) {
         // ------------------------------------------------------------------------------ K and V
         Ring ring = {0, 0};
-        const int kbox = 1 << min(a.shift, 7), vbox = min(1 << a.shift, C::VKEYS);
-        while (next_item(a, walk, C::ROWS, kBK, it)) {
+        const int kbox = min(1 << a.shift, BK), vbox = min(1 << a.shift, C::VKEYS);
+        while (next_item(a, walk, C::ROWS, BK, it)) {
             const int n = it.li.n, count = it.b1 - it.b0;
             const int entries = (int)(((unsigned)n + (1u << a.shift) - 1u) >> a.shift);
             const int32_t* tab = a.table + (size_t)it.list * a.max_pages;
@@ -168,11 +136,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 return page;
             };
             // table entries ride in registers: 32 from `win`, 32 after them (the next K block may lie there), 32 ahead
-            int win = (int)(((long long)it.b0 * kBK) >> a.shift) & ~31;
+            int win = (int)(((long long)it.b0 * BK) >> a.shift) & ~31;
             int e0 = entry(win + lane), e1 = entry(win + 32 + lane), e2 = entry(win + 64 + lane);
-            // block by block: the K chunks of block j + LEAD - 1, then the V chunks of block j
-            for (int j = 1 - C::LEAD; j < count; ++j) {
-                const int at = (int)(((long long)(it.b0 + max(j, 0)) * kBK) >> a.shift);
+            // block by block: K of block j + kLead - 1, then V of block j
+            for (int j = 1 - kLead; j < count; ++j) {
+                const int at = (int)(((long long)(it.b0 + max(j, 0)) * BK) >> a.shift);
                 if (at >= win + 32) {
                     win += 32;
                     e0 = e1;
@@ -182,11 +150,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll 1
                 for (int i = 0; i < C::PER_BLOCK; ++i) {
                     const bool is_v = i >= C::KC;
-                    const int jj = is_v ? j : j + C::LEAD - 1, c = is_v ? i - C::KC : i;
+                    const int jj = is_v ? j : j + kLead - 1, c = is_v ? i - C::KC : i;
                     if (jj < 0 || jj >= count) continue;
-                    // `rows` keys from key0 into one slot in boxes of `box`; channels 64 c .. (K) or all of them (V)
-                    const int key0 = (it.b0 + jj) * kBK + (is_v ? c * C::VKEYS : 0);
-                    const int rows = is_v ? C::VKEYS : kBK, box = is_v ? vbox : kbox, wide = is_v ? D / 64 : 1;
+                    // `rows` keys from key0 and `wide` times 64 channels into one slot, in boxes of `box` keys
+                    const int key0 = (it.b0 + jj) * BK + (is_v ? c * C::VKEYS : 0);
+                    const int rows = is_v ? C::VKEYS : BK, box = is_v ? vbox : kbox, wide = is_v ? D / 64 : C::KW;
                     if (ok) ok = mbar_wait(empty(ring.slot), ring.phase ^ 1, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) continue;
@@ -194,15 +162,15 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     const int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
                     if (lane == 0) mbar_arrive_expect_tx(full(ring.slot), (uint32_t)(act * box * 128 * wide));
                     __syncwarp();
-                    const uint32_t dst = s_ring + ring.slot * kSlot;
+                    const uint32_t dst = s_ring + ring.slot * C::SLOT;
                     const int boxes = act * wide;
                     for (int x0 = 0; x0 < boxes; x0 += 32) {
-                        const int x = x0 + lane, sub = x / wide, ch = is_v ? x % wide : c;
+                        const int x = x0 + lane, sub = x / wide, w = x % wide;
                         const int key = key0 + sub * box, e = (key >> a.shift) - win;
                         const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
                         if (x < boxes) {
-                            const uint32_t to = dst + (uint32_t)((is_v ? ch * rows * 128 : 0) + sub * box * 128);
-                            tma_load_3d(to, is_v ? &v_map : &k_map, full(ring.slot), ch * 64, key & ((1 << a.shift) - 1), e < 32 ? p0 : p1);
+                            const uint32_t to = dst + (uint32_t)(w * rows * 128 + sub * box * 128);
+                            tma_load_3d(to, is_v ? &v_map : &k_map, full(ring.slot), (is_v ? w : c * C::KW + w) * 64, key & ((1 << a.shift) - 1), e < 32 ? p0 : p1);
                         }
                     }
                     ring.next(NS);
@@ -215,114 +183,106 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 mbar_drain(full(s), 1);
             }
         __syncwarp();
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------------------ MMA issuer
+    } else if (warp <= C::TILES) {
+        // ------------------------------------------------------------------------------ MMA issuer of a row tile
         // The whole warp runs this loop in step, and one lane issues (see umma_bf16_warp).
+        const int t = warp - 1;
         const uint32_t leader = elect_one();
-        const uint32_t idesc_s = umma_idesc_bf16_m128(kBK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
-        const uint64_t q_desc = umma_desc_k_sw128(s_q), k_desc = umma_desc_k_sw128(s_ring);
+        const uint32_t idesc_s = umma_idesc_bf16_m128(BK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
+        const uint64_t q_desc = umma_desc_k_sw128(s_q + t * C::Q_TILE), k_desc = umma_desc_k_sw128(s_ring);
         const uint64_t v_desc = umma_desc_mn_sw128(s_ring, C::VKEYS * 128);
-        uint32_t p_phase = 0, q_phase = 0;              // bit t: parity of the next phase of p_full(t), q_full(t)
-        Ring ring = {0, 0}, k_ring = {0, 0}, v_ring = {0, 0};
-        while (next_item(a, walk, C::ROWS, kBK, it)) {
+        uint32_t p_phase = 0, q_phase = 0;              // bit b: parity of the next phase of p_full(t, b)
+        Ring ring = {0, 0};
+        while (next_item(a, walk, C::ROWS, BK, it)) {
             const int count = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
-            const int rows = it.li.rows_tok * a.G - it.tile * C::ROWS;
-            const int nt = __shfl_sync(0xffffffffu, C::TILES == 2 && rows > 128 ? 2 : 1, 0);
-            for (int t = 0; t < nt; ++t) {
-                if (ok) ok = mbar_wait(q_full(t), (q_phase >> t) & 1, abort_flag);
-                q_phase ^= 1u << t;
-            }
+            const int nt = __shfl_sync(0xffffffffu, C::TILES == 2 && it.li.rows_tok * a.G - it.tile * C::ROWS > 128 ? 2 : 1, 0);
+            if (t >= nt) {                              // nothing to do with these blocks but to give their slots back
 #pragma unroll 1
-            for (int j = -C::LEAD; j < count; ++j)
-#pragma unroll 1
-                for (int t = 0; t < nt; ++t) {
-                    // (both row tiles read a block: the first waits for its slots, the last gives them back)
-                    const bool first = t == 0, last = t == nt - 1;
-                    const int buf = C::TILES == 2 ? t : j & 1;
-                    if (j >= 0) {                       // O += P(j) V(j)
-                        if (ok) ok = mbar_wait(p_full(buf), (p_phase >> buf) & 1, abort_flag);
-                        Ring r = first ? ring : v_ring;
-                        if (first) v_ring = ring;
-#pragma unroll
-                        for (int c = 0; c < C::VC; ++c) {
-                            if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
-                            ok = __all_sync(0xffffffffu, ok);
-                            if (ok) {
-                                tc_fence_after_sync();
-                                const uint64_t vd = v_desc + r.slot * (kSlot >> 4);
-                                const uint32_t pa = tmem + buf * 128 + c * (C::VKEYS / 2);
-#pragma unroll
-                                for (int ks = 0; ks < C::VKEYS / 16; ++ks) {
-                                    if (c * C::VKEYS + ks * 16 == kBK / 2) {
-                                        ok = __all_sync(0xffffffffu, mbar_wait(p_rest(buf), (p_phase >> buf) & 1, abort_flag));
-                                        tc_fence_after_sync();
-                                    }
-                                    umma_bf16_ts_warp(leader, tmem + C::O_COL + t * D, pa + ks * 8, vd + ks * (2048 >> 4), idesc_o,
-                                                      c + ks > 0 ? 1u : (uint32_t)j);
-                                }
-                                if (last) umma_commit_warp(leader, empty(r.slot));
-                            }
-                            r.next(NS);
-                        }
-                        p_phase ^= 1u << buf;
-                        if (first) ring = r;
-                        if (ok) umma_commit_warp(leader, o_done(t));
-                    }
-                    if (j + C::LEAD < count) {          // S(j + LEAD) = Q K^T, over the P just used
-                        Ring r = first ? ring : k_ring;
-                        if (first) k_ring = ring;
-#pragma unroll
-                        for (int c = 0; c < C::KC; ++c) {
-                            if (first && ok) ok = mbar_wait(full(r.slot), r.phase, abort_flag);
-                            ok = __all_sync(0xffffffffu, ok);
-                            if (ok) {
-                                tc_fence_after_sync();
-                                const uint64_t qd = q_desc + (t * C::Q_TILE + c * 16384u) / 16, kd = k_desc + r.slot * (kSlot >> 4);
-#pragma unroll
-                                for (int ks = 0; ks < 4; ++ks)
-                                    umma_bf16_warp(leader, tmem + buf * 128, qd + ks * 2, kd + ks * 2, idesc_s, c + ks > 0 ? 1u : 0u);
-                                if (last) umma_commit_warp(leader, empty(r.slot));
-                            }
-                            r.next(NS);
-                        }
-                        if (first) ring = r;
-                        if (ok) umma_commit_warp(leader, s_full(buf));
-                    }
+                for (int i = 0; i < count * C::PER_BLOCK; ++i) {
+                    if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
+                    if (leader) mbar_arrive(empty(ring.slot));
+                    ring.next(NS);
                 }
+                ok = __all_sync(0xffffffffu, ok);
+                continue;
+            }
+            if (ok) ok = mbar_wait(q_full(t), q_phase, abort_flag);
+            q_phase ^= 1;
+#pragma unroll 1
+            for (int j = -kLead; j < count; ++j) {
+                const int b = j & 1;
+                const uint32_t s_tmem = tmem + (2 * t + b) * BK;
+                if (j >= 0) {                           // O += P(j) V(j)
+                    if (ok) ok = mbar_wait(p_full(t, b), (p_phase >> b) & 1, abort_flag);
+                    p_phase ^= 1u << b;
+#pragma unroll
+                    for (int c = 0; c < C::VC; ++c) {
+                        if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (ok) {
+                            tc_fence_after_sync();
+                            const uint64_t vd = v_desc + ring.slot * (C::SLOT >> 4);
+#pragma unroll
+                            for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+                                umma_bf16_ts_warp(leader, tmem + C::O_COL + t * D, s_tmem + (c * C::VKEYS + ks * 16) / 2, vd + ks * (2048 >> 4),
+                                                  idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
+                            umma_commit_warp(leader, empty(ring.slot));
+                        }
+                        ring.next(NS);
+                    }
+                    if (ok) umma_commit_warp(leader, o_done(t));
+                }
+                if (j + kLead < count) {                // S(j + kLead) = Q K^T, over the P just used
+#pragma unroll
+                    for (int c = 0; c < C::KC; ++c) {
+                        if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (ok) {
+                            tc_fence_after_sync();
+                            const uint64_t qd = q_desc + c * C::KW * (16384 >> 4), kd = k_desc + ring.slot * (C::SLOT >> 4);
+#pragma unroll
+                            for (int ks = 0; ks < 4 * C::KW; ++ks)
+                                umma_bf16_warp(leader, s_tmem, qd + (ks / 4) * (16384 >> 4) + ks % 4 * 2, kd + (ks / 4) * (BK * 128 >> 4) + ks % 4 * 2,
+                                               idesc_s, c + ks > 0 ? 1u : 0u);
+                            umma_commit_warp(leader, empty(ring.slot));
+                        }
+                        ring.next(NS);
+                    }
+                    if (ok) umma_commit_warp(leader, s_full(t, b));
+                }
+            }
         }
         if (!ok) {                                      // MMAs in flight end before the tensor memory goes back
-            umma_commit_warp(leader, drained);
-            mbar_drain(drained, 0);
+            umma_commit_warp(leader, drained(t));
+            mbar_drain(drained(t), 0);
         }
         __syncwarp();
-    }
-    } else {
-        if (C::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-        // ------------------------------------------------------------------------------ softmax, two threads per row
-        // Warps w and w + 4 of a row tile share its 32 rows: one takes keys 0-63 of a block, the other 64-127 (half the
-        // chain of instructions between scores and weights, and four warps per scheduler to fill the pipes).  They agree
-        // on the maximum through shared memory.
-        const int t = (warp - 4) / 8, half = ((warp - 4) >> 2) & 1, quarter = warp & 3;
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------------------ softmax
+        // With two row tiles four warps have one each, a thread per row; with one, warps w and w + 4 share its rows, one
+        // taking keys 0-63 of a block, the other 64-127, and agree on the maximum through shared memory.
+        const int t = C::TILES == 2 ? (warp - 4) / 4 : 0, half = C::HALVES == 2 ? (warp - 4) / 4 : 0, quarter = warp & 3;
+        constexpr int TILE_THREADS = 128 * C::HALVES;
         const int row = quarter * 32 + lane;            // tensor-memory lanes follow warp % 4
-        const int pair = 1 + t * 4 + quarter;           // named barrier of the two warps
+        const int tid = threadIdx.x - 128 - t * 128;    // among the tile's threads
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * (D / 2);
-        float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS) + t * 512;
-        uint32_t n_s[2] = {0, 0}, n_o = 0, turn = 0;
+        constexpr int OWN = D / C::HALVES;              // output channels of a thread
+        const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * OWN;
+        float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS);
+        uint32_t s_phase = 0, n_o = 0, turn = 0;
         long long seq = 0;                              // ring slots of the items before this one
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
         // any score but does not make NaN of a masked one (-infinity)
         const float scale = a.scale_log2 == 0.f ? 1e-37f : fabsf(a.scale_log2);
-        const float inv_scale = 1.f / scale;
         // the partner's value of a pair of threads (both call it, `turn` alternates the buffers)
         auto partner = [&](float mine) {
             float* at = stats + (turn & 1) * 256;
             at[half * 128 + row] = mine;
-            bar_sync(pair, 64);
+            bar_sync(1 + quarter, 64);
             ++turn;
             return at[(half ^ 1) * 128 + row];
         };
-        while (next_item(a, walk, C::ROWS, kBK, it)) {
+        while (next_item(a, walk, C::ROWS, BK, it)) {
             const ListInfo& li = it.li;
             const int count = it.b1 - it.b0;
             const int live_rows = li.rows_tok * a.G - it.tile * C::ROWS;
@@ -333,8 +293,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
             // ---- queries: 16 bytes per thread and step, rows without a query are zero
             const int head0 = (it.list - quotient(it.list, a.div_hkv) * a.Hkv) * a.G;
-            const int row0 = it.tile * C::ROWS + t * 128, tid = threadIdx.x - 128 - t * 256;
-            constexpr int PIECES = D / 8, STEPS = 128 * PIECES / 256, BATCH = STEPS < 8 ? STEPS : 8;
+            const int row0 = it.tile * C::ROWS + t * 128;
+            constexpr int PIECES = D / 8, STEPS = 128 * PIECES / TILE_THREADS, BATCH = STEPS < 8 ? STEPS : 8;
             // (the same thread that stored an output piece in this place, so the place is free)
             const uint32_t q_tile = s_q + t * C::Q_TILE;
             auto q_place = [&](int r, int piece) { return q_tile + (piece / 8) * 16384u + r * 128u + (((piece % 8) * 16u) ^ ((r & 7) * 16u)); };
@@ -343,7 +303,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 uint4 v[BATCH];
 #pragma unroll
                 for (int i = 0; i < BATCH; ++i) {
-                    const int at = (i0 + i) * 256 + tid, r = at / PIECES, piece = at % PIECES;
+                    const int at = (i0 + i) * TILE_THREADS + tid, r = at / PIECES, piece = at % PIECES;
                     const int tok = quotient(row0 + r, a.div_g), h = head0 + row0 + r - tok * a.G;
                     v[i] = make_uint4(0, 0, 0, 0);
                     if (tok < li.rows_tok)
@@ -351,7 +311,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 }
 #pragma unroll
                 for (int i = 0; i < BATCH; ++i) {
-                    const int at = (i0 + i) * 256 + tid;
+                    const int at = (i0 + i) * TILE_THREADS + tid;
                     if (a.scale_log2 < 0.f) {
                         v[i].x ^= 0x80008000u;
                         v[i].y ^= 0x80008000u;
@@ -372,38 +332,36 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             const int seen = limit_of(li, a, quotient(row0, a.div_g));
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < count; ++j) {
-                const int key0 = (it.b0 + j) * kBK;
-                const int buf = C::TILES == 2 ? t : j & 1;
-                if (ok) ok = mbar_wait(s_full(buf), n_s[buf] & 1, abort_flag);
-                ++n_s[buf];
+                const int key0 = (it.b0 + j) * BK, b = j & 1;
+                if (ok) ok = mbar_wait(s_full(t, b), (s_phase >> b) & 1, abort_flag);
+                s_phase ^= 1u << b;
                 ok = __all_sync(0xffffffffu, ok);
-                if (key0 + kBK > li.n && t == 0) {
-                    // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN:
-                    // each half makes its own zero before its weights let the product go.  (A parity tells two neighbouring phases apart: with
-                    // scores a block ahead, the slots' earlier use is only known to be over when the product before is.)
-                    if (C::TILES == 1 && j > 0 && ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
+                if (key0 + BK > li.n) {
+                    // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN: they become
+                    // zero before the weights let the product go (by both tiles: the zeros are the same).  (A parity tells two neighbouring phases apart: with scores
+                    // ahead, the slots' earlier use is only known to be over when the product before is.)
+                    if (j > 0 && ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
                     for (int c = 0; c < C::VC; ++c) {
                         const long long at = seq + C::v_at(j, count) + c;
                         const uint32_t s = (uint32_t)(at % NS);
-                        const int from = max(half * 64, li.n - key0) - c * C::VKEYS, to = half * 64 + 64 - c * C::VKEYS;
-                        const int r0 = max(from, 0), r1 = min(to, C::VKEYS);
-                        if (r0 >= r1) continue;
+                        const int from = max(0, li.n - key0 - c * C::VKEYS);
+                        if (from >= C::VKEYS) continue;
                         if (ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
-                        for (int i = tid & 127; i < (r1 - r0) * PIECES; i += 128) {
-                            const int r = r0 + i / PIECES, piece = i % PIECES;
-                            sts128(s_ring + s * kSlot + (piece / 8) * (C::VKEYS * 128u) + r * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
+                        for (int i = tid; i < (C::VKEYS - from) * PIECES; i += TILE_THREADS) {
+                            const int r = from + i / PIECES, piece = i % PIECES;
+                            sts128(s_ring + s * C::SLOT + (piece / 8) * (C::VKEYS * 128u) + r * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
                         }
                     }
                     fence_proxy_async_smem();
                 }
                 __syncwarp();
                 tc_fence_after_sync();
-                const uint32_t s_col = tmem + lanes + buf * 128;
+                const uint32_t s_col = tmem + lanes + (2 * t + b) * BK;
                 uint32_t x[2][32];
                 tmem_ld_x32(s_col + half * 64, x[0]);
                 tmem_ld_x32(s_col + half * 64 + 32, x[1]);
                 tmem_ld_wait();
-                if (key0 + kBK > seen) {
+                if (key0 + BK > seen) {
                     const int local = lim - key0 - half * 64;
 #pragma unroll
                     for (int i = 0; i < 64; ++i)
@@ -418,87 +376,69 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         top[i] = max3(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + e]), __uint_as_float(x[i / 2][i % 2 * 16 + e + 1]));
                     top[i] = fmaxf(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + 15]));
                 }
-                tc_fence_before_sync();                 // the partner's weights go over scores read here
-                const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                const float m_blk = fmaxf(mine, partner(mine)) * scale;
-                tc_fence_after_sync();
-                bool move = false;
-                float f = 1.f;
-                if (m == -INFINITY) {
-                    m = ceilf(m_blk);                   // nothing seen so far: sum and output are zero
-                } else if (m_blk > m + kRescale) {
-                    const float up = ceilf(m_blk);
-                    f = ex2(m - up);
-                    l *= f;
-                    m = up;
-                    move = true;
+                float raw = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                if (C::HALVES == 2) {
+                    tc_fence_before_sync();             // the partner's weights go over scores read here
+                    raw = fmaxf(raw, partner(raw));
+                    tc_fence_after_sync();
                 }
+                const float m_blk = raw * scale;
+                const bool move = m_blk > m + kRescale; // (a row that has seen nothing has m = -infinity)
                 if (__any_sync(0xffffffffu, move)) {
-                    // (j > 0: m was finite.)  The product of the block before must have ended.
+                    const float f = move ? ex2(m - m_blk) : 1.f;
+                    l *= f;
+                    if (move) m = m_blk;
+                    if (j > 0) {
+                    // the product of the block before must have ended
                     if (ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
                     ok = __all_sync(0xffffffffu, ok);
                     tc_fence_after_sync();
 #pragma unroll 1
-                    for (int c = 0; c < D / 2; c += 16) {
-                        uint32_t o[16];
-                        tmem_ld_x16(o_col + c, o);
+                    for (int c = 0; c < OWN; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld_x32(o_col + c, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st_x16(o_col + c, o);
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st_x32(o_col + c, o);
+                    }
                     }
                 }
+                // The epilogue waits for the product of the last block, and can tell it from the one before only if that has
+                // ended when the last weights are let go.
+                if (j > 0 && j + 1 == count) {
+                    if (ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                }
+                // The two tiles take turns on the exponential unit (per scheduler: warps w and w + 4 are on the same one), so
+                // that the loads, maxima and waits of one run beside the exponentials of the other.
+                if (nt == 2 && (t == 1 || j > 0)) bar_sync(7 + t * 4 + quarter, 64);
                 const float z = m == -INFINITY ? 0.f : m;
                 const float2 c2 = make_float2(scale, scale), z2 = make_float2(-z, -z);
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                // the polynomial's range reduction wants small whole z and no masked score
-                if (__all_sync(0xffffffffu, key0 + kBK <= seen && fabsf(z) < 1048576.f)) {
-                    const Exp2Poly e2(scale, inv_scale, z);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t p[16];
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t p[16];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float2 y = make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1]));
-                            if (POLY(e / 2)) {
-                                y = e2(y);
-                            } else {
-                                y = fma2(y, c2, z2);
-                                y.x = ex2(y.x);
-                                y.y = ex2(y.y);
-                            }
-                            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
-                            p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
-                        }
-                        tmem_st_x16(s_col + half * 32 + i * 16, p);
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
+                        y.x = ex2(y.x);
+                        y.y = ex2(y.y);
+                        sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
+                        p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
-                            y.x = ex2(y.x);
-                            y.y = ex2(y.y);
-                            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
-                            p[e / 2] = pack_bf16(y.x, y.y);
-                        }
-                        tmem_st_x16(s_col + half * 32 + i * 16, p);
-                    }
+                    tmem_st_x16(s_col + half * 32 + i * 16, p);
                 }
+                if (nt == 2 && (t == 0 || j + 1 < count)) bar_arrive(7 + (t ^ 1) * 4 + quarter, 64);
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(half == 0 ? p_full(buf) : p_rest(buf));
+                if (lane == 0) mbar_arrive(p_full(t, b));
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
-            // ---- output: each half its channels
-            l += partner(l);
+            // ---- output: with two threads per row each its channels
+            if (C::HALVES == 2) l += partner(l);
             n_o += (uint32_t)count;
-            // (a parity tells two neighbouring phases apart.  With scores a block ahead, all that is known here is that
-            // the product of two blocks before the last has ended, so its successor is waited for on its own)
-            if (C::TILES == 1 && count > 1 && ok) ok = mbar_wait(o_done(t), (n_o - 2) & 1, abort_flag);
             if (ok) ok = mbar_wait(o_done(t), (n_o - 1) & 1, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after_sync();
@@ -508,7 +448,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 // through shared memory (where the queries were: every product with them has ended), so that rows leave
                 // in one piece
 #pragma unroll 1
-                for (int c = 0; c < D / 2; c += 32) {
+                for (int c = 0; c < OWN; c += 32) {
                     uint32_t o[32];
                     tmem_ld_x32(o_col + c, o);
                     tmem_ld_wait();
@@ -519,13 +459,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
                         v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
                         v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                        sts128(q_place(row, (half * (D / 2) + c + e) / 8), v);
+                        sts128(q_place(row, (half * OWN + c + e) / 8), v);
                     }
                 }
-                bar_sync(9 + t, 256);
+                bar_sync(5 + t, TILE_THREADS);
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i) {
-                    const int at = i * 256 + tid, r = at / PIECES, piece = at % PIECES;
+                    const int at = i * TILE_THREADS + tid, r = at / PIECES, piece = at % PIECES;
                     const int tk = quotient(row0 + r, a.div_g), h = head0 + row0 + r - tk * a.G;
                     if (tk < li.rows_tok)
                         *reinterpret_cast<uint4*>(a.out + ((size_t)(li.q0 + tk) * a.Hq + h) * D + piece * 8) = lds128(q_place(r, piece));
@@ -536,13 +476,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 const size_t slot = (size_t)2 * blockIdx.x + (it.first ? 0 : 1);
                 float* dst = a.part_o + slot * C::ROWS * D + (t * 128 + row) * 4;
 #pragma unroll 1
-                for (int c = 0; c < D / 2; c += 32) {
+                for (int c = 0; c < OWN; c += 32) {
                     uint32_t o[32];
                     tmem_ld_x32(o_col + c, o);
                     tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4*>(dst + (half * (D / 2) + c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        *reinterpret_cast<uint4*>(dst + (half * OWN + c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 }
                 if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * C::ROWS + t * 128 + row) * 2) = make_float2(m, l);
             }
@@ -571,7 +511,7 @@ ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& arg
     a.part_o = static_cast<float*>(ctx->workspace);
     a.part_ml = a.part_o + (size_t)2 * kPagedMaxCtas * C::ROWS * D;
     CUtensorMap k_map, v_map;
-    const uint32_t kbox = (uint32_t)s.page_rows, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
+    const uint32_t kbox = s.page_rows < C::BK ? (uint32_t)s.page_rows : (uint32_t)C::BK, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
     if (!ea_paged_map(ctx, s, k_pages, kbox, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_chunk_kernel<D>;
     EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
@@ -579,7 +519,7 @@ ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& arg
     ea_count_launches(ctx, 1);
     ea_status err = EA_CHECK_LAUNCH();
     if (err != EA_OK) return err;
-    return ea_launch_paged_combine(ctx, s, a, C::ROWS, kBK, ctas, st);
+    return ea_launch_paged_combine(ctx, s, a, C::ROWS, C::BK, ctas, st);
 }
 
 }  // namespace
