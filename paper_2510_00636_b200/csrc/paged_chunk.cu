@@ -2,12 +2,12 @@
 //
 // A CTA works on row tiles of 128 packed rows (row = token * G + head), two of them at head_dim <= 128, one at 256 (the
 // output of a tile takes head_dim of the 512 tensor-memory columns), against blocks of 64 (two tiles) or 128 keys:
-//     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory, two buffers per tile
-//     P = 2^(c S - m)  running maximum m and sum l per row; P (bf16) over S in tensor memory
+//     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
+//     P = 2^(c S - m)  running maximum m and sum l per row; P (bf16) in tensor memory, two buffers per tile
 //     O += P V         A = P from tensor memory, B = V as it lies (rows are the contraction index: MN-major)
 // One warp keeps K and V flowing through a ring of slots (TMA boxes of a page each), one warp per row tile issues its MMAs
 // (the waits of one are hidden by the other's), eight warps do the softmax, 64 scores per thread and block.  The scores of
-// the next block are there when the softmax of one ends.
+// the next block are on their way as soon as those of this one have been read.
 //
 // The running maximum only moves when a row's scores exceed it by more than 2^8 (the weights then stay within fp32 and
 // bf16 range, and the sum, which uses the same maximum, cancels it): O is rescaled in tensor memory only then.
@@ -22,7 +22,6 @@ using namespace ptx;
 namespace {
 
 constexpr float kRescale = 8.0f;
-constexpr int kLead = 2;                                // blocks that the scores run ahead of the product
 
 template <int D> struct Chunk {
     static constexpr int TILES = D == 256 ? 1 : 2;
@@ -37,16 +36,16 @@ template <int D> struct Chunk {
     static constexpr uint32_t Q_TILE = 128u * D * 2;
     static constexpr int NSLOT = D == 64 ? 20 : D == 128 ? 10 : 9;
     static constexpr int THREADS = 128 + 256;           // warps 0 (loads), 1 and 2 (MMA of a row tile), an idle one, the softmax warps
-    static constexpr int BARS = 2 * NSLOT + 14;
+    static constexpr int BARS = 2 * NSLOT + 16;
     static constexpr int TAIL_WALK = BARS * 8 + 16;
     static constexpr int TAIL_STATS = TAIL_WALK + (int)sizeof(Walk);
     static constexpr int TAIL = TAIL_STATS + (HALVES == 2 ? 2 * 2 * 128 * 4 : 0);      // [turn][half][row]
     static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)SLOT + TAIL;
-    static constexpr uint32_t O_COL = 256;              // tensor memory: S (P) of tile t, buffer b at (2 t + b) BK, O from 256
+    static constexpr uint32_t O_COL = 256;              // tensor memory: S of tile t at 2 t BK, P of buffer b BK + b BK / 2 on, O from 256
     static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
     static_assert(KC * KW * 64 == D && VC * VKEYS == BK && VKEYS % 16 == 0, "slots");
     // Order of the blocks in the ring: K0 K1 V0 K2 V1 ...; where block j's V begins, in slots after the item's first
-    static __device__ __forceinline__ int v_at(int j, int count) { return (j + kLead < count ? j + kLead : count) * KC + j * VC; }
+    static __device__ __forceinline__ int v_at(int j, int count) { return (j + 2 < count ? j + 2 : count) * KC + j * VC; }
 };
 
 // A place in the ring: slot, and the parity of its use.
@@ -73,12 +72,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     uint8_t* tail = gen + C::TILES * C::Q_TILE + NS * C::SLOT;
     auto full = [&](uint32_t s) { return bars + 8u * s; };
     auto empty = [&](uint32_t s) { return bars + 8u * (NS + s); };
-    // per row tile t and score buffer b
-    auto s_full = [&](int t, int b) { return bars + 8u * (2 * NS + 2 * t + b); };
+    // per row tile t (and buffer b of the weights): scores written, scores read, weights written, product done
+    auto s_full = [&](int t) { return bars + 8u * (2 * NS + t); };
+    auto s_read = [&](int t) { return bars + 8u * (2 * NS + 2 + t); };
     auto p_full = [&](int t, int b) { return bars + 8u * (2 * NS + 4 + 2 * t + b); };
-    auto o_done = [&](int t) { return bars + 8u * (2 * NS + 8 + t); };
-    auto q_full = [&](int t) { return bars + 8u * (2 * NS + 10 + t); };
-    auto drained = [&](int t) { return bars + 8u * (2 * NS + 12 + t); };      // only used when a wait has given up
+    auto o_done = [&](int t, int b) { return bars + 8u * (2 * NS + 8 + 2 * t + b); };
+    auto q_full = [&](int t) { return bars + 8u * (2 * NS + 12 + t); };
+    auto drained = [&](int t) { return bars + 8u * (2 * NS + 14 + t); };      // only used when a wait has given up
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * C::BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
     Walk* start = reinterpret_cast<Walk*>(tail + C::TAIL_WALK);
@@ -91,10 +91,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         }
         for (int t = 0; t < 2; ++t) {
             for (int b = 0; b < 2; ++b) {
-                mbar_init(s_full(t, b), 1);
                 mbar_init(p_full(t, b), 4 * C::HALVES);
+                mbar_init(o_done(t, b), 1);
             }
-            mbar_init(o_done(t), 1);
+            mbar_init(s_full(t), 1);
+            mbar_init(s_read(t), 4 * C::HALVES);
             mbar_init(q_full(t), 4 * C::HALVES);
             mbar_init(drained(t), 1);
         }
@@ -138,8 +139,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             // table entries ride in registers: 32 from `win`, 32 after them (the next K block may lie there), 32 ahead
             int win = (int)(((long long)it.b0 * BK) >> a.shift) & ~31;
             int e0 = entry(win + lane), e1 = entry(win + 32 + lane), e2 = entry(win + 64 + lane);
-            // block by block: K of block j + kLead - 1, then V of block j
-            for (int j = 1 - kLead; j < count; ++j) {
+            // block by block: K of block j + 1, then V of block j
+            for (int j = -1; j < count; ++j) {
                 const int at = (int)(((long long)(it.b0 + max(j, 0)) * BK) >> a.shift);
                 if (at >= win + 32) {
                     win += 32;
@@ -150,7 +151,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll 1
                 for (int i = 0; i < C::PER_BLOCK; ++i) {
                     const bool is_v = i >= C::KC;
-                    const int jj = is_v ? j : j + kLead - 1, c = is_v ? i - C::KC : i;
+                    const int jj = is_v ? j : j + 1, c = is_v ? i - C::KC : i;
                     if (jj < 0 || jj >= count) continue;
                     // `rows` keys from key0 and `wide` times 64 channels into one slot, in boxes of `box` keys
                     const int key0 = (it.b0 + jj) * BK + (is_v ? c * C::VKEYS : 0);
@@ -191,7 +192,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const uint32_t idesc_s = umma_idesc_bf16_m128(BK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
         const uint64_t q_desc = umma_desc_k_sw128(s_q + t * C::Q_TILE), k_desc = umma_desc_k_sw128(s_ring);
         const uint64_t v_desc = umma_desc_mn_sw128(s_ring, C::VKEYS * 128);
-        uint32_t p_phase = 0, q_phase = 0;              // bit b: parity of the next phase of p_full(t, b)
+        const uint32_t s_tmem = tmem + 2 * t * BK, o_tmem = tmem + C::O_COL + t * D;
+        uint32_t p_phase = 0, q_phase = 0, r_phase = 0; // parity of the next phase of p_full(t, b) (bit b), q_full, s_read
         Ring ring = {0, 0};
         while (next_item(a, walk, C::ROWS, BK, it)) {
             const int count = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
@@ -209,30 +211,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             if (ok) ok = mbar_wait(q_full(t), q_phase, abort_flag);
             q_phase ^= 1;
 #pragma unroll 1
-            for (int j = -kLead; j < count; ++j) {
-                const int b = j & 1;
-                const uint32_t s_tmem = tmem + (2 * t + b) * BK;
-                if (j >= 0) {                           // O += P(j) V(j)
-                    if (ok) ok = mbar_wait(p_full(t, b), (p_phase >> b) & 1, abort_flag);
-                    p_phase ^= 1u << b;
-#pragma unroll
-                    for (int c = 0; c < C::VC; ++c) {
-                        if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (ok) {
-                            tc_fence_after_sync();
-                            const uint64_t vd = v_desc + ring.slot * (C::SLOT >> 4);
-#pragma unroll
-                            for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-                                umma_bf16_ts_warp(leader, tmem + C::O_COL + t * D, s_tmem + (c * C::VKEYS + ks * 16) / 2, vd + ks * (2048 >> 4),
-                                                  idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
-                            umma_commit_warp(leader, empty(ring.slot));
-                        }
-                        ring.next(NS);
+            for (int j = -1; j < count; ++j) {
+                if (j + 1 < count) {                    // S = Q K(j + 1)^T, once the softmax has read the scores before
+                    if (j >= 0) {
+                        if (ok) ok = mbar_wait(s_read(t), r_phase, abort_flag);
+                        r_phase ^= 1;
                     }
-                    if (ok) umma_commit_warp(leader, o_done(t));
-                }
-                if (j + kLead < count) {                // S(j + kLead) = Q K^T, over the P just used
 #pragma unroll
                     for (int c = 0; c < C::KC; ++c) {
                         if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
@@ -248,7 +232,28 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         }
                         ring.next(NS);
                     }
-                    if (ok) umma_commit_warp(leader, s_full(t, b));
+                    if (ok) umma_commit_warp(leader, s_full(t));
+                }
+                if (j >= 0) {                           // O += P(j) V(j)
+                    const int b = j & 1;
+                    if (ok) ok = mbar_wait(p_full(t, b), (p_phase >> b) & 1, abort_flag);
+                    p_phase ^= 1u << b;
+#pragma unroll
+                    for (int c = 0; c < C::VC; ++c) {
+                        if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (ok) {
+                            tc_fence_after_sync();
+                            const uint64_t vd = v_desc + ring.slot * (C::SLOT >> 4);
+                            const uint32_t p_tmem = s_tmem + BK + b * (BK / 2) + c * (C::VKEYS / 2);
+#pragma unroll
+                            for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+                                umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + ks * (2048 >> 4), idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
+                            umma_commit_warp(leader, empty(ring.slot));
+                        }
+                        ring.next(NS);
+                    }
+                    if (ok) umma_commit_warp(leader, o_done(t, b));
                 }
             }
         }
@@ -269,7 +274,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         constexpr int OWN = D / C::HALVES;              // output channels of a thread
         const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * OWN;
         float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS);
-        uint32_t s_phase = 0, n_o = 0, turn = 0;
+        uint32_t s_phase = 0, turn = 0, uses[2] = {0, 0};   // uses: of the weights' buffers, before this item
         long long seq = 0;                              // ring slots of the items before this one
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
         // any score but does not make NaN of a masked one (-infinity)
@@ -331,16 +336,20 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             // keys that every row of the tile sees
             const int seen = limit_of(li, a, quotient(row0, a.div_g));
             float m = -INFINITY, l = 0.f;
+            // the product of block j has ended
+            auto wait_product = [&](int j) {
+                if (ok) ok = mbar_wait(o_done(t, j & 1), (uses[j & 1] + (uint32_t)(j >> 1)) & 1, abort_flag);
+                __syncwarp();
+            };
             for (int j = 0; j < count; ++j) {
                 const int key0 = (it.b0 + j) * BK, b = j & 1;
-                if (ok) ok = mbar_wait(s_full(t, b), (s_phase >> b) & 1, abort_flag);
-                s_phase ^= 1u << b;
-                ok = __all_sync(0xffffffffu, ok);
+                if (ok) ok = mbar_wait(s_full(t), s_phase, abort_flag);
+                s_phase ^= 1;
                 if (key0 + BK > li.n) {
                     // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN: they become
-                    // zero before the weights let the product go (by both tiles: the zeros are the same).  (A parity tells two neighbouring phases apart: with scores
-                    // ahead, the slots' earlier use is only known to be over when the product before is.)
-                    if (j > 0 && ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
+                    // zero before the weights let the product go (by both tiles: the zeros are the same).  (A parity tells two
+                    // neighbouring phases apart: the slots' earlier use is known to be over when the product before is.)
+                    if (j > 0) wait_product(j - 1);
                     for (int c = 0; c < C::VC; ++c) {
                         const long long at = seq + C::v_at(j, count) + c;
                         const uint32_t s = (uint32_t)(at % NS);
@@ -356,11 +365,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 }
                 __syncwarp();
                 tc_fence_after_sync();
-                const uint32_t s_col = tmem + lanes + (2 * t + b) * BK;
+                const uint32_t s_col = tmem + lanes + 2 * t * BK;
                 uint32_t x[2][32];
                 tmem_ld_x32(s_col + half * 64, x[0]);
                 tmem_ld_x32(s_col + half * 64 + 32, x[1]);
-                tmem_ld_wait();
+                tmem_ld_wait();                         // (of the whole warp)
+                tc_fence_before_sync();
+                if (lane == 0 && j + 1 < count) mbar_arrive(s_read(t));
                 if (key0 + BK > seen) {
                     const int local = lim - key0 - half * 64;
 #pragma unroll
@@ -377,11 +388,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     top[i] = fmaxf(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + 15]));
                 }
                 float raw = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                if (C::HALVES == 2) {
-                    tc_fence_before_sync();             // the partner's weights go over scores read here
-                    raw = fmaxf(raw, partner(raw));
-                    tc_fence_after_sync();
-                }
+                if (C::HALVES == 2) raw = fmaxf(raw, partner(raw));
                 const float m_blk = raw * scale;
                 const bool move = m_blk > m + kRescale; // (a row that has seen nothing has m = -infinity)
                 if (__any_sync(0xffffffffu, move)) {
@@ -389,27 +396,21 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     l *= f;
                     if (move) m = m_blk;
                     if (j > 0) {
-                    // the product of the block before must have ended
-                    if (ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
-                    tc_fence_after_sync();
+                        wait_product(j - 1);
+                        tc_fence_after_sync();
 #pragma unroll 1
-                    for (int c = 0; c < OWN; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld_x32(o_col + c, o);
-                        tmem_ld_wait();
+                        for (int c = 0; c < OWN; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld_x32(o_col + c, o);
+                            tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st_x32(o_col + c, o);
-                    }
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st_x32(o_col + c, o);
+                        }
                     }
                 }
-                // The epilogue waits for the product of the last block, and can tell it from the one before only if that has
-                // ended when the last weights are let go.
-                if (j > 0 && j + 1 == count) {
-                    if (ok) ok = mbar_wait(o_done(t), (n_o + (uint32_t)j - 1) & 1, abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
-                }
+                // (the buffer that these weights go to is free: the scores of this block were issued, and so have ended, after
+                // the product of two blocks before)
                 // The two tiles take turns on the exponential unit (per scheduler: warps w and w + 4 are on the same one), so
                 // that the loads, maxima and waits of one run beside the exponentials of the other.
                 if (nt == 2 && (t == 1 || j > 0)) bar_sync(7 + t * 4 + quarter, 64);
@@ -427,20 +428,19 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
                         p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
                     }
-                    tmem_st_x16(s_col + half * 32 + i * 16, p);
+                    tmem_st_x16(s_col + BK + b * (BK / 2) + half * 32 + i * 16, p);
                 }
                 if (nt == 2 && (t == 0 || j + 1 < count)) bar_arrive(7 + (t ^ 1) * 4 + quarter, 64);
                 tmem_st_wait();
                 tc_fence_before_sync();
-                __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(t, b));
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
             // ---- output: with two threads per row each its channels
             if (C::HALVES == 2) l += partner(l);
-            n_o += (uint32_t)count;
-            if (ok) ok = mbar_wait(o_done(t), (n_o - 1) & 1, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
+            wait_product(count - 1);
+            uses[0] += (uint32_t)(count + 1) / 2;
+            uses[1] += (uint32_t)count / 2;
             tc_fence_after_sync();
             const bool whole = it.b0 == 0 && it.b1 == it.blocks;
             const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
