@@ -195,6 +195,7 @@ class Context:
         _check(lib().ea_create(ctypes.byref(handle), self.device.index or 0, int(workspace_bytes)),
                "ea_create")
         self._h = handle
+        self.device_index = self.device.index or 0
         self.workspace_bytes = int(workspace_bytes)
 
     @classmethod
@@ -652,6 +653,8 @@ def ea_compress_host(ctx: Context, shape: Shape, q_win, k, v, pos_next, n_future
 
 
 # ---- paged cache -----------------------------------------------------------------------------------------------------
+# One generation step makes these calls once per layer, so their checks are kept short: one pass over each tensor, raw
+# addresses and the raw stream.
 def make_paged_shape(n_seqs, n_q_heads, n_kv_heads, head_dim, page_rows, n_pages, max_pages) -> PagedShape:
     return PagedShape(n_seqs, n_q_heads, n_kv_heads, head_dim, page_rows, n_pages, max_pages)
 
@@ -663,33 +666,31 @@ def ea_paged_workspace_bytes(shape: PagedShape, max_q: int = 1) -> int:
     return int(out.value)
 
 
-def _sized(t, dtype, name, *sizes):
-    _dev_tensor(t, dtype, name)
-    if tuple(t.shape) != sizes:
+def _address(t, dtype, sizes, device, name):
+    """Device address of a contiguous tensor of the given type, sizes and device (None: any sizes)."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() < 0 or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+    if sizes is not None and t.shape != sizes:
         raise ValueError(f"{name}: expected shape {list(sizes)}, got {list(t.shape)}")
-    return t
+    if t.get_device() != device:
+        raise ValueError(f"{name}: a tensor on {t.device} in a call of a context on cuda:{device}")
+    return t.data_ptr()
 
 
-def _on_device(ctx, *tensors):
-    for t in tensors:
-        if t is not None and t.device.index != (ctx.device.index or 0):
-            raise ValueError(f"a tensor on {t.device} in a call of a context on {ctx.device}")
+def _raw_stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _pools(shape, k_pages, v_pages):
-    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        _sized(t, torch.bfloat16, name, shape.n_pages, shape.page_rows, shape.head_dim)
-
-
-def _slot_outputs(shape, order, n_slots, slots, offsets, device):
+def _slot_map(shape, order, n_slots, slots, offsets, device):
+    """(slots, offsets) as given or new, and their addresses."""
+    n = (shape.n_seqs if order == SLOTS_BY_TOKEN else shape.n_seqs * shape.n_kv_heads) + 1
     if slots is None:
-        slots = torch.empty(int(n_slots), dtype=torch.int32, device=device)
+        slots = torch.empty(int(n_slots), dtype=torch.int32, device=f"cuda:{device}")
     elif slots.dim() != 1:
         raise ValueError("slots: expected one dimension")
-    n = (shape.n_seqs if order == SLOTS_BY_TOKEN else shape.n_seqs * shape.n_kv_heads) + 1
     if offsets is None:
-        offsets = torch.empty(n, dtype=torch.int32, device=device)
-    return _dev_tensor(slots, torch.int32, "slots"), _sized(offsets, torch.int32, "offsets", n)
+        offsets = torch.empty(n, dtype=torch.int32, device=f"cuda:{device}")
+    return slots, offsets, _address(slots, torch.int32, None, device, "slots"), _address(offsets, torch.int32, (n,), device, "offsets")
 
 
 def ea_page_plan(ctx: Context, shape: PagedShape, old_lens, new_lens, block_table, free_pages, n_free, n_slots=None,
@@ -697,90 +698,90 @@ def ea_page_plan(ctx: Context, shape: PagedShape, old_lens, new_lens, block_tabl
     """Takes and gives back pages as the lists' lengths (int32 [S,Hkv]) change; ``block_table`` int32 [S,Hkv,max_pages],
     ``free_pages`` int32 [n_pages] and ``n_free`` int32 [1] are updated.  With ``n_slots`` (capacity of the slot map) or
     ``slots`` returns (slots, offsets) of the new rows, else None."""
-    S, Hkv = shape.n_seqs, shape.n_kv_heads
-    _sized(old_lens, torch.int32, "old_lens", S, Hkv)
-    _sized(new_lens, torch.int32, "new_lens", S, Hkv)
-    _sized(block_table, torch.int32, "block_table", S, Hkv, shape.max_pages)
-    _sized(free_pages, torch.int32, "free_pages", shape.n_pages)
-    _sized(n_free, torch.int32, "n_free", 1)
+    S, Hkv, dev, i32 = shape.n_seqs, shape.n_kv_heads, ctx.device_index, torch.int32
+    a_old = _address(old_lens, i32, (S, Hkv), dev, "old_lens")
+    a_new = _address(new_lens, i32, (S, Hkv), dev, "new_lens")
+    a_table = _address(block_table, i32, (S, Hkv, shape.max_pages), dev, "block_table")
+    a_free = _address(free_pages, i32, (shape.n_pages,), dev, "free_pages")
+    a_count = _address(n_free, i32, (1,), dev, "n_free")
+    a_slots = a_off = None
+    capacity = 0
     want = n_slots is not None or slots is not None
     if want:
-        slots, offsets = _slot_outputs(shape, order, n_slots, slots, offsets, old_lens.device)
+        slots, offsets, a_slots, a_off = _slot_map(shape, order, n_slots, slots, offsets, dev)
+        capacity = slots.shape[0]
     elif offsets is not None:
         raise ValueError("offsets: given without n_slots or slots")
-    _on_device(ctx, old_lens, new_lens, block_table, free_pages, n_free, slots, offsets)
-    _check(lib().ea_page_plan(ctx._h, ctypes.byref(shape), _ptr(old_lens), _ptr(new_lens), _ptr(block_table),
-                              _ptr(free_pages), _ptr(n_free), int(order), _ptr(slots), int(slots.numel()) if want else 0,
-                              _ptr(offsets), _stream(ctx.device)), "ea_page_plan")
+    _check(lib().ea_page_plan(ctx._h, ctypes.byref(shape), a_old, a_new, a_table, a_free, a_count, order, a_slots, capacity,
+                              a_off, _raw_stream(dev)), "ea_page_plan")
     return (slots, offsets) if want else None
 
 
 def ea_page_slots(ctx: Context, shape: PagedShape, block_table, first_row, end_row, n_slots=None,
                   order: int = SLOTS_BY_LIST, slots=None, offsets=None):
     """Slots of the rows ``first_row .. end_row - 1`` (int32 [S,Hkv]) of every list -> (slots [n_slots], offsets)."""
-    S, Hkv = shape.n_seqs, shape.n_kv_heads
-    _sized(block_table, torch.int32, "block_table", S, Hkv, shape.max_pages)
-    _sized(first_row, torch.int32, "first_row", S, Hkv)
-    _sized(end_row, torch.int32, "end_row", S, Hkv)
+    S, Hkv, dev, i32 = shape.n_seqs, shape.n_kv_heads, ctx.device_index, torch.int32
+    a_table = _address(block_table, i32, (S, Hkv, shape.max_pages), dev, "block_table")
+    a_first = _address(first_row, i32, (S, Hkv), dev, "first_row")
+    a_end = _address(end_row, i32, (S, Hkv), dev, "end_row")
     if n_slots is None and slots is None:
         raise ValueError("ea_page_slots: give n_slots or slots")
-    slots, offsets = _slot_outputs(shape, order, n_slots, slots, offsets, first_row.device)
-    _on_device(ctx, block_table, first_row, end_row, slots, offsets)
-    _check(lib().ea_page_slots(ctx._h, ctypes.byref(shape), _ptr(block_table), _ptr(first_row), _ptr(end_row), int(order),
-                               _ptr(slots), int(slots.numel()), _ptr(offsets), _stream(ctx.device)), "ea_page_slots")
+    slots, offsets, a_slots, a_off = _slot_map(shape, order, n_slots, slots, offsets, dev)
+    _check(lib().ea_page_slots(ctx._h, ctypes.byref(shape), a_table, a_first, a_end, order, a_slots, slots.shape[0], a_off,
+                               _raw_stream(dev)), "ea_page_slots")
     return slots, offsets
 
 
-def _token_rows(t, name, heads, d):
-    """(data pointer holder, elements between tokens or 0, rows) of [rows, d] (dense) or [tokens, heads, d] whose tokens
-    may lie apart."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.bfloat16):
+def _token_rows(t, name, heads, d, device):
+    """(address, elements between tokens or 0, rows) of [rows, d] (dense) or [tokens, heads, d] whose tokens may lie apart."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.get_device() < 0:
         raise TypeError(f"{name}: expected a CUDA tensor of {torch.bfloat16}")
-    if t.dim() == 2 and t.shape[1] == d and t.is_contiguous():
-        return t, 0, t.shape[0]
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, d):
-        raise ValueError(f"{name}: expected [tokens, {heads}, {d}] or dense [rows, {d}], got {list(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: a tensor on {t.device} in a call of a context on cuda:{device}")
+    size = t.shape
+    if len(size) == 2 and size[1] == d and t.is_contiguous():
+        return t.data_ptr(), 0, size[0]
+    if len(size) != 3 or size[1] != heads or size[2] != d:
+        raise ValueError(f"{name}: expected [tokens, {heads}, {d}] or dense [rows, {d}], got {list(size)}")
     if t.is_contiguous():
-        return t, 0, t.shape[0] * heads
-    if t.stride(2) != 1 or t.stride(1) != d:
+        return t.data_ptr(), 0, size[0] * heads
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
         raise ValueError(f"{name}: the heads of a token must lie side by side")
-    if t.shape[0] <= 1:
-        return t, 0, t.shape[0] * heads
+    if size[0] <= 1:
+        return t.data_ptr(), 0, size[0] * heads
     if t.stride(0) < heads * d or t.stride(0) % 8 != 0:
         raise ValueError(f"{name}: tokens must not overlap and must lie a multiple of 8 elements apart")
-    return t, t.stride(0), t.shape[0] * heads
+    return t.data_ptr(), t.stride(0), size[0] * heads
 
 
 def ea_page_store(ctx: Context, shape: PagedShape, slots, k_new, v_new, k_pages, v_pages):
     """Rows ``k_new, v_new`` bf16 ([rows, d], or [tokens, Hkv, d] with tokens any distance apart) into ``slots`` int32 [rows]
     of ``k_pages, v_pages`` [n_pages, page_rows, d] (in place; -1: the row goes nowhere)."""
-    _pools(shape, k_pages, v_pages)
-    _, ks, n = _token_rows(k_new, "k_new", shape.n_kv_heads, shape.head_dim)
-    _, vs, nv = _token_rows(v_new, "v_new", shape.n_kv_heads, shape.head_dim)
+    dev, d, pool = ctx.device_index, shape.head_dim, (shape.n_pages, shape.page_rows, shape.head_dim)
+    a_kp = _address(k_pages, torch.bfloat16, pool, dev, "k_pages")
+    a_vp = _address(v_pages, torch.bfloat16, pool, dev, "v_pages")
+    a_k, ks, n = _token_rows(k_new, "k_new", shape.n_kv_heads, d, dev)
+    a_v, vs, nv = _token_rows(v_new, "v_new", shape.n_kv_heads, d, dev)
     if n != nv:
         raise ValueError("k_new and v_new differ in rows")
-    _sized(slots, torch.int32, "slots", n)
-    _on_device(ctx, slots, k_new, v_new, k_pages, v_pages)
-    _check(lib().ea_page_store(ctx._h, ctypes.byref(shape), _ptr(slots), n, _ptr(k_new), _ptr(v_new), ks, vs, _ptr(k_pages),
-                               _ptr(v_pages), _stream(ctx.device)), "ea_page_store")
+    a_slots = _address(slots, torch.int32, (n,), dev, "slots")
+    _check(lib().ea_page_store(ctx._h, ctypes.byref(shape), a_slots, n, a_k, a_v, ks, vs, a_kp, a_vp, _raw_stream(dev)),
+           "ea_page_store")
 
 
 def ea_page_load(ctx: Context, shape: PagedShape, slots, k_pages, v_pages, k_out=None, v_out=None):
     """Rows out of ``slots`` int32 [rows] -> (k, v) bf16 [rows, d]; rows with slot -1 are left as they are."""
-    _dev_tensor(slots, torch.int32, "slots")
-    _pools(shape, k_pages, v_pages)
-    n, d = slots.numel(), shape.head_dim
-    if k_out is None:
-        k_out = torch.empty((n, d), dtype=torch.bfloat16, device=slots.device)
-    if v_out is None:
-        v_out = torch.empty((n, d), dtype=torch.bfloat16, device=slots.device)
-    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
-        _dev_tensor(t, torch.bfloat16, name)
-        if t.numel() != n * d:
-            raise ValueError(f"{name}: expected {n} rows of {d}")
-    _on_device(ctx, slots, k_pages, v_pages, k_out, v_out)
-    _check(lib().ea_page_load(ctx._h, ctypes.byref(shape), _ptr(slots), n, _ptr(k_pages), _ptr(v_pages), _ptr(k_out),
-                              _ptr(v_out), _stream(ctx.device)), "ea_page_load")
+    dev, d, pool = ctx.device_index, shape.head_dim, (shape.n_pages, shape.page_rows, shape.head_dim)
+    a_slots = _address(slots, torch.int32, None, dev, "slots")
+    a_kp = _address(k_pages, torch.bfloat16, pool, dev, "k_pages")
+    a_vp = _address(v_pages, torch.bfloat16, pool, dev, "v_pages")
+    n = slots.numel()
+    k_out = k_pages.new_empty((n, d)) if k_out is None else k_out
+    v_out = k_pages.new_empty((n, d)) if v_out is None else v_out
+    a_k, a_v = (_address(t, torch.bfloat16, None, dev, name) for t, name in ((k_out, "k_out"), (v_out, "v_out")))
+    if k_out.numel() != n * d or v_out.numel() != n * d:
+        raise ValueError(f"k_out, v_out: expected {n} rows of {d}")
+    _check(lib().ea_page_load(ctx._h, ctypes.byref(shape), a_slots, n, a_kp, a_vp, a_k, a_v, _raw_stream(dev)), "ea_page_load")
     return k_out, v_out
 
 
@@ -789,25 +790,22 @@ def ea_paged_attention(ctx: Context, shape: PagedShape, q, q_offsets, max_q: int
     """Attention of new tokens ``q`` bf16 [T,Hq,d] (tokens any distance apart; sequence s owns ``q_offsets[s] ..
     q_offsets[s+1]``, int32 [S+1], at most ``max_q`` tokens each) over the lists of ``kv_lens`` int32 [S,Hkv] rows ->
     out bf16 [T,Hq,d] (and lse fp32 [T,Hq] if asked).  The new tokens' own pairs are the last rows of the lists."""
-    S, Hq, Hkv, d = shape.n_seqs, shape.n_q_heads, shape.n_kv_heads, shape.head_dim
-    if not (isinstance(q, torch.Tensor) and q.dim() == 3):
+    S, Hq, Hkv, d, dev, i32 = shape.n_seqs, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, ctx.device_index, torch.int32
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError(f"q: expected [tokens, {Hq}, {d}]")
-    _, stride, rows = _token_rows(q, "q", Hq, d)
-    T = q.shape[0]
-    _sized(q_offsets, torch.int32, "q_offsets", S + 1)
-    _sized(kv_lens, torch.int32, "kv_lens", S, Hkv)
-    _sized(block_table, torch.int32, "block_table", S, Hkv, shape.max_pages)
-    _pools(shape, k_pages, v_pages)
-    if out is None:
-        out = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device)
+    a_q, stride, _ = _token_rows(q, "q", Hq, d, dev)
+    T, pool = q.shape[0], (shape.n_pages, shape.page_rows, d)
+    a_off = _address(q_offsets, i32, (S + 1,), dev, "q_offsets")
+    a_lens = _address(kv_lens, i32, (S, Hkv), dev, "kv_lens")
+    a_table = _address(block_table, i32, (S, Hkv, shape.max_pages), dev, "block_table")
+    a_kp = _address(k_pages, torch.bfloat16, pool, dev, "k_pages")
+    a_vp = _address(v_pages, torch.bfloat16, pool, dev, "v_pages")
+    out = k_pages.new_empty((T, Hq, d)) if out is None else out
+    a_out = _address(out, torch.bfloat16, (T, Hq, d), dev, "out")
     if lse is None and want_lse:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-    _sized(out, torch.bfloat16, "out", T, Hq, d)
-    if lse is not None:
-        _sized(lse, torch.float32, "lse", T, Hq)
-    _on_device(ctx, q, q_offsets, kv_lens, block_table, k_pages, v_pages, out, lse)
-    _check(lib().ea_paged_attention(ctx._h, ctypes.byref(shape), _ptr(q), stride, T, _ptr(q_offsets), int(max_q),
-                                    _ptr(kv_lens), _ptr(block_table), _ptr(k_pages), _ptr(v_pages),
-                                    float(d ** -0.5 if scale is None else scale), int(bool(causal)), _ptr(out), _ptr(lse),
-                                    _stream(ctx.device)), "ea_paged_attention")
+        lse = k_pages.new_empty((T, Hq), dtype=torch.float32)
+    a_lse = None if lse is None else _address(lse, torch.float32, (T, Hq), dev, "lse")
+    _check(lib().ea_paged_attention(ctx._h, ctypes.byref(shape), a_q, stride, T, a_off, max_q, a_lens, a_table, a_kp, a_vp,
+                                    d ** -0.5 if scale is None else scale, bool(causal), a_out, a_lse, _raw_stream(dev)),
+           "ea_paged_attention")
     return (out, lse) if lse is not None else out

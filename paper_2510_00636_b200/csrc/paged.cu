@@ -16,6 +16,7 @@
 namespace {
 
 constexpr int kSelfScanLists = 4096;      // up to here every CTA scans the lengths itself (48 KiB of prefixes)
+constexpr int kScanSmem = 3 * (kSelfScanLists + 1) * 4;
 constexpr int kOneCtaSlots = 8192;        // up to here a plan is one CTA's work
 constexpr int kClusterSlots = 65536;      // up to here it is one cluster's (one launch); beyond, three launches over all SMs
 constexpr int kScanThreads = 1024, kMoveThreads = 256;
@@ -334,13 +335,17 @@ ea_status launch_plan(const ea_ctx* ctx, PlanArgs a, cudaStream_t st) {
     const long long want = (quads + kMoveThreads - 1) / kMoveThreads, cap = (long long)ctx->sm_count * 4;
     const unsigned slot_grid = (unsigned)(want < 1 ? 1 : want < cap ? want : cap);
     if (few && !resize) {
-        EA_CUDA_TRY(cudaFuncSetAttribute(page_slots_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        static std::atomic<uint64_t> done{0};
+        const ea_status err = ea_allow_smem(page_slots_kernel<true>, kScanSmem, ctx->device, done);
+        if (err != EA_OK) return err;
         page_slots_kernel<true><<<slot_grid, kMoveThreads, smem, st>>>(a);
         ea_count_launches(ctx, 1);
         return EA_CHECK_LAUNCH();
     }
     if (few && a.slot_capacity <= kClusterSlots) {
-        EA_CUDA_TRY(cudaFuncSetAttribute(page_plan_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        static std::atomic<uint64_t> done{0};
+        const ea_status err = ea_allow_smem(page_plan_cluster_kernel, kScanSmem, ctx->device, done);
+        if (err != EA_OK) return err;
         // without slots nothing bounds the pages that move but the pool, so that form gets the wide cluster
         const unsigned ctas = a.slots && a.slot_capacity <= kOneCtaSlots ? 1 : 8;
         cudaLaunchConfig_t cfg = {};

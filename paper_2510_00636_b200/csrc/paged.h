@@ -1,7 +1,20 @@
 // Shared by the translation units of the paged cache.
 #pragma once
 
+#include <atomic>
+
 #include "ea_internal.h"
+
+// Lets a kernel use more than 48 KiB of dynamic shared memory: once per device (a runtime call that a generation step
+// would otherwise pay at each layer); `done` belongs to the kernel.
+template <class Kernel>
+static inline ea_status ea_allow_smem(Kernel kernel, int bytes, int device, std::atomic<uint64_t>& done) {
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return EA_OK;
+    EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (device < 64) done.fetch_or(bit, std::memory_order_release);
+    return EA_OK;
+}
 
 ea_status ea_check_paged_shape(const ea_paged_shape* s);
 // Workspace of ea_paged_attention (partial results of lists that several CTAs share).

@@ -408,10 +408,12 @@ ea_status launch_few(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs&
     const uint32_t box = s.page_rows < 64 ? (uint32_t)s.page_rows : 64u;
     if (!ea_paged_map(ctx, s, k_pages, box, &k_map) || !ea_paged_map(ctx, s, v_pages, box, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_few_kernel<D>;
-    EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    static std::atomic<uint64_t> done{0};
+    ea_status err = ea_allow_smem(kernel, C::SMEM, ctx->device, done);
+    if (err != EA_OK) return err;
     kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
     ea_count_launches(ctx, 1);
-    ea_status err = EA_CHECK_LAUNCH();
+    err = EA_CHECK_LAUNCH();
     if (err != EA_OK) return err;
     return ea_launch_paged_combine(ctx, s, a, 16, C::BK, ctas, st);
 }

@@ -514,10 +514,12 @@ ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& arg
     const uint32_t kbox = s.page_rows < C::BK ? (uint32_t)s.page_rows : (uint32_t)C::BK, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
     if (!ea_paged_map(ctx, s, k_pages, kbox, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_chunk_kernel<D>;
-    EA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    static std::atomic<uint64_t> done{0};
+    ea_status err = ea_allow_smem(kernel, C::SMEM, ctx->device, done);
+    if (err != EA_OK) return err;
     kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
     ea_count_launches(ctx, 1);
-    ea_status err = EA_CHECK_LAUNCH();
+    err = EA_CHECK_LAUNCH();
     if (err != EA_OK) return err;
     return ea_launch_paged_combine(ctx, s, a, C::ROWS, C::BK, ctas, st);
 }
