@@ -18,24 +18,27 @@ namespace {
 // takes an equal, contiguous share of all key blocks of the call, whatever list they belong to (lengths differ by list);
 // a list that several CTAs share leaves partial results (maximum, sum, unnormalised output) for paged_combine_kernel.
 //
-// Inside a CTA one warp keeps TMA boxes of K and V (128-byte swizzle) flowing into a ring, and each of NW warps owns 16
-// keys of every block: scores (mma.sync m16n8k16, 16 rows are one tile), softmax with its own running maximum, and
-// the product with its 16 value rows.  No barrier among the warps until the list ends, where they are merged in a fixed
-// order.  At most 16 of the 128 rows of a tcgen05 tile would be in use here, and the limit is memory.
+// Inside a CTA one warp keeps TMA boxes of K and V (128-byte swizzle) flowing into a ring, and each of four warps owns 16
+// keys of a block: scores (mma.sync m16n8k16, 16 rows are one tile), softmax with its own running maximum, and
+// the product with its 16 value rows.  At head_dim <= 128 a second group of four warps takes every other block: a block is a
+// chain of some 1300 cycles for a warp, about as long as its bytes take to arrive.  No barrier among the warps until the
+// list ends, where they are merged in a fixed order.  At most 16 of the 128 rows of a tcgen05 tile would be in use here,
+// and the limit is memory.
 template <int D> struct Few {
-    static constexpr int NW = D == 64 ? 8 : 4;
-    static constexpr int BK = NW * 16;                       // keys per block
+    static constexpr int GROUPS = D == 256 ? 1 : 2;
+    static constexpr int NW = 4 * GROUPS;
+    static constexpr int BK = 64;                            // keys per block
     static constexpr int CHUNKS = D / 64;
     static constexpr int CHUNK_BYTES = BK * 128;             // 64 channels of a block
     static constexpr int STAGE = 2 * CHUNKS * CHUNK_BYTES;
-    static constexpr int NST = 196608 / STAGE;               // 192 KiB in flight
     static constexpr int MERGE = NW / 2 * 16 * D * 4;
+    static constexpr int NST = (229376 - MERGE) / STAGE;     // 192 KiB in flight, or nearly
     static constexpr int THREADS = NW * 32 + 32;
     // behind the ring and the merge buffer: barriers, abort flag, range, and [NW][16] maxima and sums
     static constexpr int TAIL_ML = 16 * NST + 64;
     static constexpr int TAIL = TAIL_ML + NW * 16 * 8;
     static constexpr int SMEM = 1024 /* alignment */ + NST * STAGE + MERGE + TAIL;
-    static_assert(SMEM + 1024 <= 232448, "a CTA's shared memory, with room for static arrays");
+    static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
 };
 
 template <int D>
@@ -55,11 +58,11 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     float* ml = reinterpret_cast<float*>(tail + C::TAIL_ML);                             // [NW][16][2]
     static_assert(16 + sizeof(Walk) <= 64, "flag and range fit before the maxima");
 
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::NST; ++s) {
             mbar_init(full(s), 1);
-            mbar_init(empty(s), C::NW);
+            mbar_init(empty(s), 4);
         }
         *abort_flag = 0;
         fence_mbar_init();
@@ -78,6 +81,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         const int box_shift = a.shift < 6 ? a.shift : 6;                 // rows per box: a page, at most 64
         const int box_rows = 1 << box_shift;
         const int subs = C::BK >> box_shift;
+        const uint32_t leader = elect_one();
         while (next_item(a, walk, 16, C::BK, it)) {
             const ListInfo& li = it.li;
             const int r = it.list, b0 = it.b0;
@@ -112,18 +116,17 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 const int rest = li.n - b * C::BK;
                 int act = rest <= 0 ? 0 : (rest + box_rows - 1) >> box_shift;
                 if (act > subs) act = subs;
-                if (lane == 0) mbar_arrive_expect_tx(full(s), (uint32_t)(act * C::CHUNKS * 2 * box_rows * 128));
+                if (leader) mbar_arrive_expect_tx(full(s), (uint32_t)(act * C::CHUNKS * 2 * box_rows * 128));
                 __syncwarp();
-                const uint32_t dst = base + (uint32_t)(s * C::STAGE);
-                const int boxes = act * C::CHUNKS * 2;
-                for (int i0 = 0; i0 < boxes; i0 += 32) {
-                    const int i = i0 + lane;
-                    const int sub = i / (C::CHUNKS * 2), c = i % C::CHUNKS, kv = (i / C::CHUNKS) & 1;
-                    const int key = b * C::BK + (sub << box_shift);
+                uint32_t to = base + (uint32_t)(s * C::STAGE);
+#pragma unroll 1
+                for (int sub = 0; sub < act; ++sub, to += (uint32_t)box_rows * 128u) {
+                    const int key = b * C::BK + (sub << box_shift), y = key & ((1 << a.shift) - 1);
                     const int page = __shfl_sync(0xffffffffu, cur, ((key >> a.shift) - win) & 31);
-                    if (i < boxes) {
-                        const uint32_t to = dst + (uint32_t)((kv * C::CHUNKS + c) * C::CHUNK_BYTES + (sub << box_shift) * 128);
-                        tma_load_3d(to, kv ? &v_map : &k_map, full(s), c * 64, key & ((1 << a.shift) - 1), page);
+#pragma unroll
+                    for (int c = 0; c < C::CHUNKS; ++c) {
+                        tma_load_3d_warp(leader, to + c * C::CHUNK_BYTES, &k_map, full(s), c * 64, y, page);
+                        tma_load_3d_warp(leader, to + (C::CHUNKS + c) * C::CHUNK_BYTES, &v_map, full(s), c * 64, y, page);
                     }
                 }
             }
@@ -141,8 +144,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         const int g8 = lane >> 2, t4 = lane & 3;
         // ldmatrix row addresses inside a stage (K: keys by channels; V: transposed on the way)
         const int lm = lane >> 3, lr = lane & 7;
-        const uint32_t k_row = (uint32_t)(warp * 16 + (lm >> 1) * 8 + lr) * 128u;
-        const uint32_t v_row = (uint32_t)(warp * 16 + (lm & 1) * 8 + lr) * 128u;
+        const int group = warp / 4, slice = warp % 4 * 16;
+        const uint32_t k_row = (uint32_t)(slice + (lm >> 1) * 8 + lr) * 128u;
+        const uint32_t v_row = (uint32_t)(slice + (lm & 1) * 8 + lr) * 128u;
         const uint32_t sw = (uint32_t)lr << 4;
         while (next_item(a, walk, 16, C::BK, it)) {
             const ListInfo& li = it.li;
@@ -174,8 +178,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             for (int b = b0; b < it.b1; ++b, ++block_no) {
                 const int s = (int)(block_no % C::NST);
                 const uint32_t use = (uint32_t)(block_no / C::NST);
+                if (C::GROUPS == 2 && (block_no & 1) != group) continue;
                 if (ok) ok = mbar_wait(full(s), use & 1, abort_flag);
-                const int key0 = b * C::BK + warp * 16;
+                const int key0 = b * C::BK + slice;
                 if (key0 < li.n) {
                     const uint32_t ks_base = base + (uint32_t)(s * C::STAGE);
                     float x0[4] = {0.f, 0.f, 0.f, 0.f}, x1[4] = {0.f, 0.f, 0.f, 0.f};
@@ -376,17 +381,22 @@ __global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, in
         if (row >= live) continue;
         const float* src = a.part_o + (p0 - row0) * D + (size_t)(col * ROWS) + (row0 + row) * 4;
         const float* next = a.part_o + (p1 - row0) * D + (size_t)(col * ROWS) + (row0 + row) * 4;
-        float4 o = *reinterpret_cast<const float4*>(src);
-        const float w0 = weight[row][0];
-        o = make_float4(o.x * w0, o.y * w0, o.z * w0, o.w * w0);
-#pragma unroll 8
-        for (int p = 1; p < parts; ++p) {
-            const float w = weight[row][p];
-            const float4 v = *reinterpret_cast<const float4*>(next + (size_t)(p - 1) * 2 * ROWS * D);
-            o.x += v.x * w;
-            o.y += v.y * w;
-            o.z += v.z * w;
-            o.w += v.w * w;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int b = 0; b < parts; b += 8) {             // eight loads on their way at a time
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (b + k < parts) v[k] = __ldcg(reinterpret_cast<const float4*>(b + k == 0 ? src : next + (size_t)(b + k - 1) * 2 * ROWS * D));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float w = b + k < parts ? weight[row][b + k] : 0.f;
+                o.x += v[k].x * w;
+                o.y += v[k].y * w;
+                o.z += v[k].z * w;
+                o.w += v[k].w * w;
+            }
         }
         const int pr = tile * ROWS + row0 + row, tok = quotient(pr, a.div_g);
         const size_t at = (size_t)(li.q0 + tok) * a.Hq + head0 + pr - tok * a.G;

@@ -120,6 +120,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     if (warp == 0) {
         // ------------------------------------------------------------------------------ K and V
         Ring ring = {0, 0};
+        const uint32_t leader = elect_one();
         const int kbox = min(1 << a.shift, BK), vbox = min(1 << a.shift, C::VKEYS);
         while (next_item(a, walk, C::ROWS, BK, it)) {
             const int n = it.li.n, count = it.b1 - it.b0;
@@ -161,17 +162,22 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     if (!ok) continue;
                     const int rest = n - key0;
                     const int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
-                    if (lane == 0) mbar_arrive_expect_tx(full(ring.slot), (uint32_t)(act * box * 128 * wide));
+                    if (leader) mbar_arrive_expect_tx(full(ring.slot), (uint32_t)(act * box * 128 * wide));
                     __syncwarp();
-                    const uint32_t dst = s_ring + ring.slot * C::SLOT;
-                    const int boxes = act * wide;
-                    for (int x0 = 0; x0 < boxes; x0 += 32) {
-                        const int x = x0 + lane, sub = x / wide, w = x % wide;
-                        const int key = key0 + sub * box, e = (key >> a.shift) - win;
+                    uint32_t to = s_ring + ring.slot * C::SLOT;
+#pragma unroll 1
+                    for (int sub = 0; sub < act; ++sub, to += (uint32_t)box * 128u) {
+                        const int key = key0 + sub * box, e = (key >> a.shift) - win, y = key & ((1 << a.shift) - 1);
                         const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
-                        if (x < boxes) {
-                            const uint32_t to = dst + (uint32_t)(w * rows * 128 + sub * box * 128);
-                            tma_load_3d(to, is_v ? &v_map : &k_map, full(ring.slot), (is_v ? w : c * C::KW + w) * 64, key & ((1 << a.shift) - 1), e < 32 ? p0 : p1);
+                        const int page = e < 32 ? p0 : p1;
+                        if (is_v) {
+#pragma unroll
+                            for (int w = 0; w < D / 64; ++w)
+                                tma_load_3d_warp(leader, to + w * C::VKEYS * 128, &v_map, full(ring.slot), w * 64, y, page);
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < C::KW; ++w)
+                                tma_load_3d_warp(leader, to + w * BK * 128, &k_map, full(ring.slot), (c * C::KW + w) * 64, y, page);
                         }
                     }
                     ring.next(NS);

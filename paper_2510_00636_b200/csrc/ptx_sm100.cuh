@@ -13,6 +13,17 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
+// 1 in one lane of a warp in step, 0 in the others.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t leader;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(leader));
+    return leader;
+}
+
 __device__ __forceinline__ uint64_t globaltimer_ns() {
     uint64_t t;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
@@ -103,6 +114,17 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
         " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+// The same load for a whole warp in step, of which one lane (`leader` != 0, see elect_one) issues.  Loads issued by several
+// lanes at once run one after the other, some 100 cycles each: their operands are moved to uniform registers lane by lane.
+__device__ __forceinline__ void tma_load_3d_warp(uint32_t leader, uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(leader)
         : "memory");
 }
 // Untiled bulk copy global -> shared; both addresses 16-byte aligned, bytes a multiple of 16.
@@ -258,15 +280,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint
 // Forms for a whole warp in step, of which one lane (`leader` != 0, see elect_one) issues: descriptors and control flow
 // then stay in uniform registers.  In a branch that only one lane takes, every operand of every MMA is moved there first,
 // which takes longer than an MMA of N = 128 runs.
-__device__ __forceinline__ uint32_t elect_one() {
-    uint32_t leader;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xffffffff;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(leader));
-    return leader;
-}
 __device__ __forceinline__ void umma_bf16_warp(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                                uint32_t accumulate) {
     asm volatile(
