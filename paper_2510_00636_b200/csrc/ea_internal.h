@@ -129,9 +129,10 @@ static inline ea_quad_form ea_eq7_form(const ea_shape& s, const float* mu_bar, c
 ea_status ea_launch_logits_simt(const ea_ctx* ctx, const ea_shape& s, const __nv_bfloat16* k,
                                 const ea_quad_form& form, float* logits, cudaStream_t st);
 
-// bf16 rank-3 TMA tensor map, box (box0 x box1 x 1), 128-byte swizzle, zero fill outside.
+// bf16 rank-3 TMA tensor map, box (box0 x box1 x box2), 128-byte swizzle, zero fill outside.
 bool ea_tensor_map_bf16_3d(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, uint64_t n2,
-                           uint64_t stride1, uint64_t stride2, uint32_t box0, uint32_t box1, bool bytes_plain = false);
+                           uint64_t stride1, uint64_t stride2, uint32_t box0, uint32_t box1, bool bytes_plain = false,
+                           uint32_t box2 = 1);
 
 // Window queries from hidden states, Q[u,h,w,:] = W_Q^h H[u,w,:] in fp32 (tcgen05 GEMM).
 bool ea_project_supported(const ea_shape& s, int d_model);

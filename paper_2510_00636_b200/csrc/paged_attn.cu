@@ -29,8 +29,7 @@ template <int D> struct Few {
     static constexpr int NW = 4 * GROUPS;
     static constexpr int BK = 64;                            // keys per block
     static constexpr int CHUNKS = D / 64;
-    static constexpr int CHUNK_BYTES = BK * 128;             // 64 channels of a block
-    static constexpr int STAGE = 2 * CHUNKS * CHUNK_BYTES;
+    static constexpr int STAGE = 2 * BK * D * 2;             // K, then V, each box after box: [chunk of 64 channels][row][128 bytes]
     static constexpr int MERGE = NW / 2 * 16 * D * 4;
     static constexpr int NST = (229376 - MERGE) / STAGE;     // 192 KiB in flight, or nearly
     static constexpr int THREADS = NW * 32 + 32;
@@ -118,17 +117,21 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 if (act > subs) act = subs;
                 if (leader) mbar_arrive_expect_tx(full(s), (uint32_t)(act * C::CHUNKS * 2 * box_rows * 128));
                 __syncwarp();
-                uint32_t to = base + (uint32_t)(s * C::STAGE);
-#pragma unroll 1
-                for (int sub = 0; sub < act; ++sub, to += (uint32_t)box_rows * 128u) {
-                    const int key = b * C::BK + (sub << box_shift), y = key & ((1 << a.shift) - 1);
-                    const int page = __shfl_sync(0xffffffffu, cur, ((key >> a.shift) - win) & 31);
+                const uint32_t to = base + (uint32_t)(s * C::STAGE);
+                int y[4];                                       // first row of each box in the pool
 #pragma unroll
-                    for (int c = 0; c < C::CHUNKS; ++c) {
-                        tma_load_3d_warp(leader, to + c * C::CHUNK_BYTES, &k_map, full(s), c * 64, y, page);
-                        tma_load_3d_warp(leader, to + (C::CHUNKS + c) * C::CHUNK_BYTES, &v_map, full(s), c * 64, y, page);
-                    }
+                for (int sub = 0; sub < 4; ++sub) {
+                    const int key = b * C::BK + (sub << box_shift);
+                    const int page = __shfl_sync(0xffffffffu, cur, ((key >> a.shift) - win) & 31);
+                    y[sub] = (page << a.shift) + (key & ((1 << a.shift) - 1));
                 }
+#pragma unroll
+                for (int sub = 0; sub < 4; ++sub)
+                    if (sub < act) {
+                        const uint32_t at = to + (uint32_t)(sub * D * 2) * (uint32_t)box_rows;
+                        tma_load_3d_warp(leader, at, &k_map, full(s), 0, y[sub], 0);
+                        tma_load_3d_warp(leader, at + C::STAGE / 2, &v_map, full(s), 0, y[sub], 0);
+                    }
             }
         }
         if (!ok && lane == 0) {
@@ -145,8 +148,11 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         // ldmatrix row addresses inside a stage (K: keys by channels; V: transposed on the way)
         const int lm = lane >> 3, lr = lane & 7;
         const int group = warp / 4, slice = warp % 4 * 16;
-        const uint32_t k_row = (uint32_t)(slice + (lm >> 1) * 8 + lr) * 128u;
-        const uint32_t v_row = (uint32_t)(slice + (lm & 1) * 8 + lr) * 128u;
+        const int box_shift = a.shift < 6 ? a.shift : 6;
+        const uint32_t chunk_bytes = 128u << box_shift;         // 64 channels of a box
+        const uint32_t box_off = (uint32_t)(slice >> box_shift) * C::CHUNKS * chunk_bytes + (uint32_t)(slice & ((1 << box_shift) - 1)) * 128u;
+        const uint32_t k_row = box_off + (uint32_t)((lm >> 1) * 8 + lr) * 128u;
+        const uint32_t v_row = box_off + (uint32_t)((lm & 1) * 8 + lr) * 128u;
         const uint32_t sw = (uint32_t)lr << 4;
         while (next_item(a, walk, 16, C::BK, it)) {
             const ListInfo& li = it.li;
@@ -188,7 +194,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     for (int ks = 0; ks < D / 16; ++ks) {
                         uint32_t kf[4];
                         const uint32_t col = (uint32_t)((ks % 4) * 32 + (lm & 1) * 16);
-                        ldmatrix_x4(ks_base + (ks / 4) * C::CHUNK_BYTES + k_row + (col ^ sw), kf);
+                        ldmatrix_x4(ks_base + (ks / 4) * chunk_bytes + k_row + (col ^ sw), kf);
                         mma_bf16(x0, qf[ks], kf[0], kf[1]);
                         mma_bf16(x1, qf[ks], kf[2], kf[3]);
                     }
@@ -228,7 +234,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                         pf[x] = pack_bf16(p0, p1);           // the weights enter the product with 8 significant bits
                         pf[x + 2] = pack_bf16(p2, p3);
                     }
-                    const uint32_t vs_base = ks_base + C::CHUNKS * C::CHUNK_BYTES;
+                    const uint32_t vs_base = ks_base + C::STAGE / 2;
                     // rows behind the list's end hold anything: a weight of zero does not silence a NaN
                     uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
                     if (key0 + 16 > li.n) {
@@ -239,7 +245,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     for (int nt = 0; nt < D / 16; ++nt) {
                         uint32_t vf[4];
                         const uint32_t col = (uint32_t)((nt % 4) * 32 + (lm >> 1) * 16);
-                        ldmatrix_x4_trans(vs_base + (nt / 4) * C::CHUNK_BYTES + v_row + (col ^ sw), vf);
+                        ldmatrix_x4_trans(vs_base + (nt / 4) * chunk_bytes + v_row + (col ^ sw), vf);
                         mma_bf16(o[2 * nt], pf, vf[0] & keep0, vf[1] & keep1);
                         mma_bf16(o[2 * nt + 1], pf, vf[2] & keep0, vf[3] & keep1);
                     }
@@ -416,7 +422,7 @@ ea_status launch_few(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs&
     a.part_ml = a.part_o + (size_t)2 * kPagedMaxCtas * 16 * D;
     CUtensorMap k_map, v_map;
     const uint32_t box = s.page_rows < 64 ? (uint32_t)s.page_rows : 64u;
-    if (!ea_paged_map(ctx, s, k_pages, box, &k_map) || !ea_paged_map(ctx, s, v_pages, box, &v_map)) return EA_ERR_CUDA;
+    if (!ea_paged_map(ctx, s, k_pages, box, D / 64, &k_map) || !ea_paged_map(ctx, s, v_pages, box, D / 64, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_few_kernel<D>;
     static std::atomic<uint64_t> done{0};
     ea_status err = ea_allow_smem(kernel, C::SMEM, ctx->device, done);
@@ -433,12 +439,11 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 }  // namespace
 
-bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t box_rows, CUtensorMap* map) {
-    const uint64_t row = (uint64_t)s.head_dim * 2, page = row * s.page_rows;
+bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t rows, uint32_t chunks, CUtensorMap* map) {
     // an empty pool is never read (list_info refuses every row of it), but a map needs an address and a size
-    const uint64_t n = s.n_pages > 0 ? (uint64_t)s.n_pages : 1;
-    return ea_tensor_map_bf16_3d(map, s.n_pages > 0 ? pages : ctx->workspace, (uint64_t)s.head_dim, (uint64_t)s.page_rows, n, row, page, 64,
-                                 box_rows);
+    const uint64_t n = (uint64_t)(s.n_pages > 0 ? s.n_pages : 1) * (uint64_t)s.page_rows;
+    return ea_tensor_map_bf16_3d(map, s.n_pages > 0 ? pages : ctx->workspace, 64, n, (uint64_t)s.head_dim / 64, (uint64_t)s.head_dim * 2,
+                                 128, 64, rows, false, chunks);
 }
 
 ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st) {

@@ -219,8 +219,9 @@ __device__ void count_units(const AttnArgs& a, int BK, int rows, int list, long 
 
 constexpr int kPagedMaxCtas = 160;             // grid of the persistent kernels, at most (one CTA per SM)
 
-// The pool as a rank-3 tensor (d, rows of a page, pages) in boxes of 64 channels x box_rows rows.
-bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t box_rows, CUtensorMap* map);
+// The pool as a rank-3 tensor (64 channels, rows of all pages, d / 64) in boxes of 64 channels x rows x chunks: a box lies in
+// shared memory as [chunk][row][128 bytes], swizzled.
+bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t rows, uint32_t chunks, CUtensorMap* map);
 // Joins what several CTAs left of a row tile.
 ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st);
 // Row tiles of 128 on the tensor cores (paged_chunk.cu).

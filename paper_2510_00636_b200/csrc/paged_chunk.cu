@@ -164,20 +164,18 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     const int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
                     if (leader) mbar_arrive_expect_tx(full(ring.slot), (uint32_t)(act * box * 128 * wide));
                     __syncwarp();
-                    uint32_t to = s_ring + ring.slot * C::SLOT;
+                    const uint32_t to = s_ring + ring.slot * C::SLOT;
 #pragma unroll 1
-                    for (int sub = 0; sub < act; ++sub, to += (uint32_t)box * 128u) {
-                        const int key = key0 + sub * box, e = (key >> a.shift) - win, y = key & ((1 << a.shift) - 1);
+                    for (int sub = 0; sub < act; ++sub) {
+                        const int key = key0 + sub * box, e = (key >> a.shift) - win;
                         const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
-                        const int page = e < 32 ? p0 : p1;
-                        if (is_v) {
-#pragma unroll
-                            for (int w = 0; w < D / 64; ++w)
-                                tma_load_3d_warp(leader, to + w * C::VKEYS * 128, &v_map, full(ring.slot), w * 64, y, page);
-                        } else {
+                        const int y = ((e < 32 ? p0 : p1) << a.shift) + (key & ((1 << a.shift) - 1));
+                        if (is_v) {                     // box after box: [64 channels][row][128 bytes] each
+                            tma_load_3d_warp(leader, to + (uint32_t)(sub * box) * (D * 2), &v_map, full(ring.slot), 0, y, 0);
+                        } else {                        // the rows of a chunk of 64 channels side by side
 #pragma unroll
                             for (int w = 0; w < C::KW; ++w)
-                                tma_load_3d_warp(leader, to + w * BK * 128, &k_map, full(ring.slot), (c * C::KW + w) * 64, y, page);
+                                tma_load_3d_warp(leader, to + w * BK * 128 + (uint32_t)(sub * box) * 128u, &k_map, full(ring.slot), 0, y, c * C::KW + w);
                         }
                     }
                     ring.next(NS);
@@ -197,7 +195,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const uint32_t leader = elect_one();
         const uint32_t idesc_s = umma_idesc_bf16_m128(BK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
         const uint64_t q_desc = umma_desc_k_sw128(s_q + t * C::Q_TILE), k_desc = umma_desc_k_sw128(s_ring);
-        const uint64_t v_desc = umma_desc_mn_sw128(s_ring, C::VKEYS * 128);
+        // V: a box of `vbox` keys after the other, in it a chunk of 64 channels after the other
+        const int vbox = min(1 << a.shift, C::VKEYS), vbits = vbox == C::VKEYS ? 31 : a.shift;
+        const uint64_t v_desc = umma_desc_mn_sw128(s_ring, (uint32_t)vbox * 128u);
+        uint64_t v_step[C::VKEYS / 16];                 // to keys 16 ks ..: box (16 ks) / vbox, row (16 ks) % vbox of it
+#pragma unroll
+        for (int ks = 0; ks < C::VKEYS / 16; ++ks)
+            v_step[ks] = (uint32_t)__shfl_sync(0xffffffffu, ((ks * 16 >> vbits) * vbox * (D * 2 - 128) + ks * 2048) >> 4, 0);
         const uint32_t s_tmem = tmem + 2 * t * BK, o_tmem = tmem + C::O_COL + t * D;
         uint32_t p_phase = 0, q_phase = 0, r_phase = 0; // parity of the next phase of p_full(t, b) (bit b), q_full, s_read
         Ring ring = {0, 0};
@@ -254,7 +258,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                             const uint32_t p_tmem = s_tmem + BK + b * (BK / 2) + c * (C::VKEYS / 2);
 #pragma unroll
                             for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-                                umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + ks * (2048 >> 4), idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
+                                umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
                             umma_commit_warp(leader, empty(ring.slot));
                         }
                         ring.next(NS);
@@ -280,6 +284,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         constexpr int OWN = D / C::HALVES;              // output channels of a thread
         const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * OWN;
         float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS);
+        const int vbox = min(1 << a.shift, C::VKEYS);   // keys of a V box
         uint32_t s_phase = 0, turn = 0, uses[2] = {0, 0};   // uses: of the weights' buffers, before this item
         long long seq = 0;                              // ring slots of the items before this one
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
@@ -364,7 +369,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         if (ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
                         for (int i = tid; i < (C::VKEYS - from) * PIECES; i += TILE_THREADS) {
                             const int r = from + i / PIECES, piece = i % PIECES;
-                            sts128(s_ring + s * C::SLOT + (piece / 8) * (C::VKEYS * 128u) + r * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
+                            sts128(s_ring + s * C::SLOT + (r / vbox) * vbox * (D * 2) + ((piece / 8) * vbox + r % vbox) * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
                         }
                     }
                     fence_proxy_async_smem();
@@ -518,7 +523,7 @@ ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& arg
     a.part_ml = a.part_o + (size_t)2 * kPagedMaxCtas * C::ROWS * D;
     CUtensorMap k_map, v_map;
     const uint32_t kbox = s.page_rows < C::BK ? (uint32_t)s.page_rows : (uint32_t)C::BK, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
-    if (!ea_paged_map(ctx, s, k_pages, kbox, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, &v_map)) return EA_ERR_CUDA;
+    if (!ea_paged_map(ctx, s, k_pages, kbox, 1, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, D / 64, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_chunk_kernel<D>;
     static std::atomic<uint64_t> done{0};
     ea_status err = ea_allow_smem(kernel, C::SMEM, ctx->device, done);

@@ -843,7 +843,8 @@ ea_status launch_mma(const ea_ctx* ctx, const ea_shape& s, const void* k, const 
 // bf16 rank-3 tensor map (innermost extent first) with a (box0 x box1 x 1) box, 128-byte swizzle,
 // zero fill outside the tensor.  Strides in bytes, multiples of 16; base 16-byte aligned.
 bool ea_tensor_map_bf16_3d(CUtensorMap* map, const void* base, uint64_t n0, uint64_t n1, uint64_t n2,
-                           uint64_t stride1, uint64_t stride2, uint32_t box0, uint32_t box1, bool bytes_plain) {
+                           uint64_t stride1, uint64_t stride2, uint32_t box0, uint32_t box1, bool bytes_plain,
+                           uint32_t box2) {
     typedef CUresult (*encode_tiled_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                         const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                         CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
@@ -863,7 +864,7 @@ bool ea_tensor_map_bf16_3d(CUtensorMap* map, const void* base, uint64_t n0, uint
     if (!fn) return false;
     const cuuint64_t dims[3] = {n0, n1, n2};
     const cuuint64_t strides[2] = {stride1, stride2};
-    const cuuint32_t box[3] = {box0, box1, 1};
+    const cuuint32_t box[3] = {box0, box1, box2};
     const cuuint32_t estr[3] = {1, 1, 1};
     // bytes_plain: 8-bit elements, rows of the box stored one after the other without swizzle
     return fn(map, bytes_plain ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
