@@ -31,7 +31,9 @@ template <int D> struct Few {
     static constexpr int CHUNKS = D / 64;
     static constexpr int STAGE = 2 * BK * D * 2;             // K, then V, each box after box: [chunk of 64 channels][row][128 bytes]
     static constexpr int MERGE = NW / 2 * 16 * D * 4;
-    static constexpr int NST = (229376 - MERGE) / STAGE;     // 192 KiB in flight, or nearly
+    // 192 KiB in flight, or nearly; a stage always belongs to the same group, which so waits for each of its uses (a parity
+    // tells only neighbouring ones apart)
+    static constexpr int NST = (229376 - MERGE) / STAGE / GROUPS * GROUPS;
     static constexpr int THREADS = NW * 32 + 32;
     // behind the ring and the merge buffer: barriers, abort flag, range, and [NW][16] maxima and sums
     static constexpr int TAIL_ML = 16 * NST + 64;
