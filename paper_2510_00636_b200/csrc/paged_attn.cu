@@ -83,6 +83,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         const int box_rows = 1 << box_shift;
         const int subs = C::BK >> box_shift;
         const uint32_t leader = elect_one();
+        const uint64_t policy = evict_first_policy();                    // every row is read once: 142 -> 127 us for 676 MB
         while (next_item(a, walk, 16, C::BK, it)) {
             const ListInfo& li = it.li;
             const int r = it.list, b0 = it.b0;
@@ -131,8 +132,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 for (int sub = 0; sub < 4; ++sub)
                     if (sub < act) {
                         const uint32_t at = to + (uint32_t)(sub * D * 2) * (uint32_t)box_rows;
-                        tma_load_3d_warp(leader, at, &k_map, full(s), 0, y[sub], 0);
-                        tma_load_3d_warp(leader, at + C::STAGE / 2, &v_map, full(s), 0, y[sub], 0);
+                        tma_load_3d_warp(leader, at, &k_map, full(s), 0, y[sub], 0, policy);
+                        tma_load_3d_warp(leader, at + C::STAGE / 2, &v_map, full(s), 0, y[sub], 0, policy);
                     }
             }
         }
