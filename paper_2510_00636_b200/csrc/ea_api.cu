@@ -135,6 +135,7 @@ ea_status ea_create(ea_ctx** out_ctx, int device, size_t workspace_bytes) {
     ctx->workspace_bytes = workspace_bytes;
     ctx->status_host = nullptr;
     ctx->status_dev = nullptr;
+    ctx->counters = nullptr;
     ctx->host_ready = false;
     ctx->profiling = false;
     ctx->launches = 0;
@@ -144,6 +145,8 @@ ea_status ea_create(ea_ctx** out_ctx, int device, size_t workspace_bytes) {
     ctx->ev_stop = new (std::nothrow) cudaEvent_t[kMaxProfileEvents];
     bool ok = ctx->ev_start && ctx->ev_stop;
     if (ok && workspace_bytes > 0) ok = cudaMalloc(&ctx->workspace, workspace_bytes) == cudaSuccess;
+    if (ok) ok = cudaMalloc((void**)&ctx->counters, kCounters * sizeof(unsigned)) == cudaSuccess;
+    if (ok) ok = cudaMemset(ctx->counters, 0, kCounters * sizeof(unsigned)) == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
     if (ok) ok = cudaHostAlloc((void**)&ctx->status_host, 2 * sizeof(int), cudaHostAllocMapped) == cudaSuccess;
     if (ok) {
         ctx->status_host[0] = ctx->status_host[1] = 0;
@@ -152,6 +155,7 @@ ea_status ea_create(ea_ctx** out_ctx, int device, size_t workspace_bytes) {
     if (!ok) {
         cudaGetLastError();
         if (ctx->workspace) cudaFree(ctx->workspace);
+        if (ctx->counters) cudaFree(ctx->counters);
         if (ctx->status_host) cudaFreeHost(ctx->status_host);
         delete[] ctx->ev_start;
         delete[] ctx->ev_stop;
@@ -170,6 +174,7 @@ ea_status ea_destroy(ea_ctx* ctx) {
     cudaGetDevice(&prev);
     cudaSetDevice(ctx->device);
     if (ctx->workspace) cudaFree(ctx->workspace);
+    if (ctx->counters) cudaFree(ctx->counters);
     if (ctx->status_host) cudaFreeHost(ctx->status_host);
     if (ctx->side_ready) {
         cudaStreamDestroy(ctx->st_side);

@@ -26,6 +26,8 @@ struct ea_ctx {
     int* status_host;    // two pinned, mapped words: [0] device kernels write EA_ERR_DEVICE_TIMEOUT (other waits
                          // give up when they see it), [1] the paged-cache calls write EA_ERR_PAGES
     int* status_dev;     // device alias of status_host
+    unsigned* counters;  // kCounters device words, zero between calls: arrivals at row tiles that several CTAs share
+                         // (ea_paged_attention; whoever is last puts its word back to zero)
     // benchmark instrumentation (ea_profile_begin / ea_profile_end)
     bool profiling;
     long long launches;          // kernels launched since ea_profile_begin
@@ -40,6 +42,7 @@ struct ea_ctx {
 };
 
 constexpr int kMaxProfileEvents = 4096;
+constexpr int kCounters = 512;
 
 // Count `n` kernel launches made on behalf of `ctx`.
 static inline void ea_count_launches(const ea_ctx* ctx, int n) {

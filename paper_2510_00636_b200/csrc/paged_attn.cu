@@ -16,7 +16,7 @@ namespace {
 // ---------------------------------------------------------------------------------------- few rows
 // Row tiles of 16: a generation step has G rows per list, and the time is that of reading K and V once.  One CTA per SM
 // takes an equal, contiguous share of all key blocks of the call, whatever list they belong to (lengths differ by list);
-// a list that several CTAs share leaves partial results (maximum, sum, unnormalised output) for paged_combine_kernel.
+// a list that several CTAs share is joined by the one of them that ends last.
 //
 // Inside a CTA one warp keeps TMA boxes of K and V (128-byte swizzle) flowing into a ring, and each of four warps owns 16
 // keys of a block: scores (mma.sync m16n8k16, 16 rows are one tile), softmax with its own running maximum, and
@@ -35,12 +35,74 @@ template <int D> struct Few {
     // tells only neighbouring ones apart)
     static constexpr int NST = (229376 - MERGE) / STAGE / GROUPS * GROUPS;
     static constexpr int THREADS = NW * 32 + 32;
-    // behind the ring and the merge buffer: barriers, abort flag, range, and [NW][16] maxima and sums
-    static constexpr int TAIL_ML = 16 * NST + 64;
+    // behind the ring and the merge buffer: barriers, flags, range, and [NW][16] maxima and sums
+    static constexpr int TAIL_ML = 16 * NST + 80;
     static constexpr int TAIL = TAIL_ML + NW * 16 * 8;
     static constexpr int SMEM = 1024 /* alignment */ + NST * STAGE + MERGE + TAIL;
+    static_assert(MERGE >= 16 * kPagedMaxCtas * 4, "the weights of the parts fit the merge buffer");
     static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
 };
+
+// Joins the parts of a tile of 16 rows, `live` of them in use: THREADS / 16 threads per row turn the parts' maxima and sums into
+// weights (in `weight`, [16][parts]), then every thread adds 4 channels of a row over the parts.
+template <int D, int THREADS>
+__device__ void join_parts(const AttnArgs& a, const Shared& sh, float* weight, int live, int row0, int q0, int head0) {
+    constexpr int LANES = THREADS / 16;
+    {
+        const int row = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+        float m = -INFINITY, l = 0.f;
+        if (row < live)
+            for (int p = lane; p < sh.parts; p += LANES) {
+                const float2 v = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + (size_t)sh.slot(p) * 16 + row);
+                const float top = fmaxf(m, v.x), z = top == -INFINITY ? 0.f : top;
+                l = l * ex2(m - z) + v.y * ex2(v.x - z);
+                m = top;
+                weight[row * kPagedMaxCtas + p] = v.x;
+            }
+        float top = m;
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float z = top == -INFINITY ? 0.f : top;
+        l *= ex2(m - z);
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+        if (row < live) {
+            const float inv = inverse_sum(l);
+            for (int p = lane; p < sh.parts; p += LANES) weight[row * kPagedMaxCtas + p] = ex2(weight[row * kPagedMaxCtas + p] - z) * inv;
+            if (lane == 0 && a.lse) {
+                const int tok = quotient(row0 + row, a.div_g);
+                a.lse[(size_t)(q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G] = lse_of(top, l);
+            }
+        }
+    }
+    bar_sync(1, THREADS);
+    const int bits = live > 8 ? 4 : live > 4 ? 3 : live > 2 ? 2 : live - 1;
+    for (int i = threadIdx.x; i < (D / 4) << bits; i += THREADS) {
+        const int row = i & ((1 << bits) - 1), col = (i >> bits) * 4;
+        if (row >= live) continue;
+        const float* src = a.part_o + (col * 16) + row * 4;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int b = 0; b < sh.parts; b += 8) {          // eight loads on their way at a time
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (b + k < sh.parts) v[k] = __ldcg(reinterpret_cast<const float4*>(src + (size_t)sh.slot(b + k) * 16 * D));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float w = b + k < sh.parts ? weight[row * kPagedMaxCtas + b + k] : 0.f;
+                o.x += v[k].x * w;
+                o.y += v[k].y * w;
+                o.z += v[k].z * w;
+                o.w += v[k].w * w;
+            }
+        }
+        const int tok = quotient(row0 + row, a.div_g);
+        const size_t at = (size_t)(q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G;
+        *reinterpret_cast<uint2*>(a.out + at * D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+    }
+}
 
 template <int D>
 __global__ void __launch_bounds__(Few<D>::THREADS, 1)
@@ -57,7 +119,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 16 * C::NST);
     Walk* start = reinterpret_cast<Walk*>(tail + 16 * C::NST + 16);
     float* ml = reinterpret_cast<float*>(tail + C::TAIL_ML);                             // [NW][16][2]
-    static_assert(16 + sizeof(Walk) <= 64, "flag and range fit before the maxima");
+    static_assert(16 + sizeof(Walk) <= 80, "flags and range fit before the maxima");
+    volatile int* last_flag = abort_flag + 1;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
@@ -305,112 +368,43 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     }
                 }
             }
-            if (warp == 0) {
-                const bool whole = b0 == 0 && it.b1 == it.blocks;
-                const size_t slot = 2 * (size_t)blockIdx.x + (it.first ? 0 : 1);
+            const bool whole = b0 == 0 && it.b1 == it.blocks;
+            if (whole) {
+                if (warp != 0) continue;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (!live[x]) continue;
-                    if (whole) {
-                        const float inv = sum[x] > 0.f ? 1.f / sum[x] : (sum[x] == 0.f ? 0.f : sum[x]);
-                        const size_t row = (size_t)(li.q0 + tok[x]) * a.Hq + hd[x];
-                        uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D) + t4;
+                    const float inv = inverse_sum(sum[x]);
+                    const size_t row = (size_t)(li.q0 + tok[x]) * a.Hq + hd[x];
+                    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D) + t4;
 #pragma unroll
-                        for (int i = 0; i < D / 8; ++i) dst[i * 4] = pack_bf16(o[i][2 * x] * inv, o[i][2 * x + 1] * inv);
-                        if (a.lse && t4 == 0) a.lse[row] = lse_of(mx[x], sum[x]);
-                    } else {
-                        // (parts: [D / 4][16 rows][4 channels])
-                        float2* dst = reinterpret_cast<float2*>(a.part_o + slot * 16 * D + ((t4 / 2) * 16 + g8 + 8 * x) * 4 + (t4 & 1) * 2);
-#pragma unroll
-                        for (int i = 0; i < D / 8; ++i) dst[i * 64] = make_float2(o[i][2 * x], o[i][2 * x + 1]);
-                        if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + g8 + 8 * x) * 2) = make_float2(mx[x], sum[x]);
-                    }
+                    for (int i = 0; i < D / 8; ++i) dst[i * 4] = pack_bf16(o[i][2 * x] * inv, o[i][2 * x + 1] * inv);
+                    if (a.lse && t4 == 0) a.lse[row] = lse_of(mx[x], sum[x]);
                 }
+                continue;
             }
+            const Shared sh = shared_by(it, walk.total, gridDim.x);
+            if (warp == 0) {
+                const size_t slot = (size_t)2 * blockIdx.x + (it.first ? 0 : 1);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!live[x]) continue;
+                    // (a part: [D / 4][16 rows][4 channels])
+                    float2* dst = reinterpret_cast<float2*>(a.part_o + slot * 16 * D + ((t4 / 2) * 16 + g8 + 8 * x) * 4 + (t4 & 1) * 2);
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) dst[i * 64] = make_float2(o[i][2 * x], o[i][2 * x + 1]);
+                    if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * 16 + g8 + 8 * x) * 2) = make_float2(mx[x], sum[x]);
+                }
+                __syncwarp();
+                if (lane == 0) *last_flag = arrives_last(a.counters + sh.c0, sh.parts) ? 1 : 0;
+            }
+            bar_sync(1, C::NW * 32);
+            if (*last_flag)
+                join_parts<D, C::NW * 32>(a, sh, merge, min(16, li.rows_tok * a.G - tile * 16), tile * 16, li.q0, head0);
         }
     }
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
-}
-
-// Joins the partial results of row tiles (ROWS rows) that several CTAs shared: one CTA per (tile, 16 of its rows, list).
-// First a warp per row turns the parts' maxima and sums into weights, then every thread adds 4 channels of a row over
-// the parts, in the order of the keys.
-template <int D, int ROWS>
-__global__ void __launch_bounds__(128) paged_combine_kernel(const AttnArgs a, int BK, int ctas) {
-    __shared__ float weight[16][kPagedMaxCtas];
-    constexpr int GROUPS = ROWS / 16;
-    const int r = blockIdx.y, tile = blockIdx.x / GROUPS, row0 = blockIdx.x % GROUPS * 16;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const ListInfo li = list_info(a, r, false);
-    const int head0 = (r - quotient(r, a.div_hkv) * a.Hkv) * a.G;
-    const int rows_left = li.rows_tok * a.G - (tile * ROWS + row0);
-    if (rows_left <= 0) return;
-    const int live = min(rows_left, 16);
-    long long before, total;
-    count_units<128>(a, BK, ROWS, r, &before, &total);
-    long long u0 = before;
-    for (int t = 0; t < tile; ++t) u0 += tile_blocks(li, a, t, ROWS, BK);
-    const long long u1 = u0 + tile_blocks(li, a, tile, ROWS, BK);
-    const Division division(total, ctas);
-    const int c0 = division.owner(u0), c1 = division.owner(u1 - 1), parts = c1 - c0 + 1;
-    if (parts == 1) return;
-    // a CTA's first item is its part 0, its last part 1: only the tile's first CTA may have begun before it
-    const size_t p0 = ((size_t)2 * c0 + (u0 > division.begin(c0) ? 1 : 0)) * ROWS + row0;
-    const size_t p1 = (size_t)2 * (c0 + 1) * ROWS + row0;                   // part 1 of the tile; the next ones 2 ROWS on
-    for (int row = warp; row < live; row += 4) {
-        float m = -INFINITY, l = 0.f;
-        for (int p = lane; p < parts; p += 32) {
-            const float2 v = *reinterpret_cast<const float2*>(a.part_ml + ((p == 0 ? p0 : p1 + (size_t)(p - 1) * 2 * ROWS) + row) * 2);
-            weight[row][p] = v.x;
-            m = fmaxf(m, v.x);
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        const float z = m == -INFINITY ? 0.f : m;
-        for (int p = lane; p < parts; p += 32) {
-            const float f = ex2(weight[row][p] - z);
-            l += f * a.part_ml[((p == 0 ? p0 : p1 + (size_t)(p - 1) * 2 * ROWS) + row) * 2 + 1];
-            weight[row][p] = f;
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-        const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-        for (int p = lane; p < parts; p += 32) weight[row][p] *= inv;
-        if (lane == 0 && a.lse) {
-            const int pr = tile * ROWS + row0 + row, tok = quotient(pr, a.div_g);
-            a.lse[(size_t)(li.q0 + tok) * a.Hq + head0 + pr - tok * a.G] = lse_of(m, l);
-        }
-    }
-    __syncthreads();
-    // (a part's rows lie side by side in pieces of 4 channels: [D / 4][ROWS][4])
-    const int bits = live > 8 ? 4 : live > 4 ? 3 : live > 2 ? 2 : live - 1;
-    for (int i = threadIdx.x; i < (D / 4) << bits; i += 128) {
-        const int row = i & ((1 << bits) - 1), col = (i >> bits) * 4;
-        if (row >= live) continue;
-        const float* src = a.part_o + (p0 - row0) * D + (size_t)(col * ROWS) + (row0 + row) * 4;
-        const float* next = a.part_o + (p1 - row0) * D + (size_t)(col * ROWS) + (row0 + row) * 4;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int b = 0; b < parts; b += 8) {             // eight loads on their way at a time
-            float4 v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (b + k < parts) v[k] = __ldcg(reinterpret_cast<const float4*>(b + k == 0 ? src : next + (size_t)(b + k - 1) * 2 * ROWS * D));
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float w = b + k < parts ? weight[row][b + k] : 0.f;
-                o.x += v[k].x * w;
-                o.y += v[k].y * w;
-                o.z += v[k].z * w;
-                o.w += v[k].w * w;
-            }
-        }
-        const int pr = tile * ROWS + row0 + row, tok = quotient(pr, a.div_g);
-        const size_t at = (size_t)(li.q0 + tok) * a.Hq + head0 + pr - tok * a.G;
-        *reinterpret_cast<uint2*>(a.out + at * D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
-    }
 }
 
 size_t few_part_floats(int d) { return (size_t)2 * kPagedMaxCtas * 16 * (d + 2); }
@@ -432,9 +426,7 @@ ea_status launch_few(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs&
     if (err != EA_OK) return err;
     kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
     ea_count_launches(ctx, 1);
-    err = EA_CHECK_LAUNCH();
-    if (err != EA_OK) return err;
-    return ea_launch_paged_combine(ctx, s, a, 16, C::BK, ctas, st);
+    return EA_CHECK_LAUNCH();
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -447,17 +439,6 @@ bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages,
     const uint64_t n = (uint64_t)(s.n_pages > 0 ? s.n_pages : 1) * (uint64_t)s.page_rows;
     return ea_tensor_map_bf16_3d(map, s.n_pages > 0 ? pages : ctx->workspace, 64, n, (uint64_t)s.head_dim / 64, (uint64_t)s.head_dim * 2,
                                  128, 64, rows, false, chunks);
-}
-
-ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st) {
-    const dim3 grid((unsigned)(((long long)a.max_q * a.G + rows - 1) / rows * (rows / 16)), (unsigned)(s.n_seqs * s.n_kv_heads));
-    const int d = s.head_dim;
-    auto kernel = rows == 16    ? (d == 64 ? paged_combine_kernel<64, 16> : d == 128 ? paged_combine_kernel<128, 16> : paged_combine_kernel<256, 16>)
-                  : rows == 128 ? paged_combine_kernel<256, 128>
-                                : (d == 64 ? paged_combine_kernel<64, 256> : paged_combine_kernel<128, 256>);
-    kernel<<<grid, 128, 0, st>>>(a, BK, ctas);
-    ea_count_launches(ctx, 1);
-    return EA_CHECK_LAUNCH();
 }
 
 // Up to 16 rows per list fit one tile of the kernel for few rows; more go to the tensor-core tiles of 128.
@@ -496,6 +477,7 @@ extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape
     a.out = static_cast<__nv_bfloat16*>(out);
     a.lse = lse_opt;
     a.status = ctx->status_dev;
+    a.counters = ctx->counters;
     a.lists = shape->n_seqs * shape->n_kv_heads;
     a.Hq = shape->n_q_heads;
     a.Hkv = shape->n_kv_heads;

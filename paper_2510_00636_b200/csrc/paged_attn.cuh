@@ -29,6 +29,7 @@ struct AttnArgs {
     float* lse;                  // [n_tokens, Hq] or nullptr
     float* part_o;               // unnormalised partial outputs, two row tiles per CTA
     float* part_ml;              // their maxima (of scores in units of log 2) and sums
+    unsigned* counters;          // arrivals at the row tiles that several CTAs share
     int* status;
     int lists, Hq, Hkv, G, shift, n_pages, max_pages, n_tokens, max_q, causal;
     FastDiv div_g, div_hkv;      // by G and by Hkv
@@ -100,12 +101,13 @@ struct Division {
 
 // A CTA's share: where it begins, and how many units it has.
 struct Walk {
-    long long count, left;
+    long long unit, total, count, left;  // next unit, units of the call, of the share, of them still to do
     int list, tile, block;
 };
 // Consecutive units of one row tile.
 struct Item {
     ListInfo li;
+    long long unit;                      // the first one's number in the call
     int list, tile, b0, b1, blocks;      // key blocks b0 .. b1 - 1 of `blocks`
     bool first;                          // the CTA's first item
 };
@@ -123,6 +125,8 @@ __device__ __forceinline__ bool next_item(const AttnArgs& a, Walk& w, int rows, 
     it.b0 = w.block;
     it.b1 = w.left < it.blocks - w.block ? w.block + (int)w.left : it.blocks;
     it.first = w.left == w.count;
+    it.unit = w.unit;
+    w.unit += it.b1 - it.b0;
     w.left -= it.b1 - it.b0;
     w.block = it.b1;
     if (w.block == it.blocks) {
@@ -164,6 +168,8 @@ __device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int cta
     const Division division(total, ctas);
     const long long first = division.begin(cta), end = division.begin(cta + 1);
     if (tid == 0) {
+        out->unit = first;
+        out->total = total;
         out->count = out->left = end - first;
         out->list = out->tile = out->block = 0;
     }
@@ -186,44 +192,40 @@ __device__ void find_range(const AttnArgs& a, int BK, int rows, int cta, int cta
     }
 }
 
-// Units of the lists before `list`, and of all.  Every thread calls it and gets both.
-template <int THREADS>
-__device__ void count_units(const AttnArgs& a, int BK, int rows, int list, long long* before, long long* total) {
-    __shared__ long long warp_before[THREADS / 32], warp_total[THREADS / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    long long b = 0, t = 0;
-    for (int r = tid; r < a.lists; r += THREADS) {
-        const ListInfo li = list_info(a, r, false);
-        const long long units = list_units(li, a, rows, BK);
-        t += units;
-        if (r < list) b += units;
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        b += __shfl_xor_sync(0xffffffffu, b, d);
-        t += __shfl_xor_sync(0xffffffffu, t, d);
-    }
-    if (lane == 0) {
-        warp_before[warp] = b;
-        warp_total[warp] = t;
-    }
-    __syncthreads();
-    b = t = 0;
-    for (int w = 0; w < THREADS / 32; ++w) {
-        b += warp_before[w];
-        t += warp_total[w];
-    }
-    *before = b;
-    *total = t;
-}
-
 constexpr int kPagedMaxCtas = 160;             // grid of the persistent kernels, at most (one CTA per SM)
+static_assert(2 * kPagedMaxCtas <= kCounters, "a counter per CTA and row tile");
+
+// The CTAs that share a row tile: `parts` of them from c0 on.  Each leaves its part (maxima, sums, unnormalised output)
+// in a slot of the workspace, and the one that arrives last joins them, in the order of the keys.  A CTA's first item
+// is its slot 0, its last slot 1; only the tile's first CTA may have begun before the tile.
+struct Shared {
+    int c0, parts, first_slot;
+    __device__ __forceinline__ int slot(int p) const { return p == 0 ? first_slot : 2 * (c0 + p); }
+};
+__device__ __forceinline__ Shared shared_by(const Item& it, long long total, int ctas) {
+    const Division d(total, ctas);
+    const long long u0 = it.unit - it.b0;
+    Shared s;
+    s.c0 = d.owner(u0);
+    s.parts = d.owner(u0 + it.blocks - 1) - s.c0 + 1;
+    s.first_slot = 2 * s.c0 + (u0 > d.begin(s.c0) ? 1 : 0);
+    return s;
+}
+// Called by one thread once the part's writers have met at a barrier: whether the other parts are all there.  (Two tiles
+// that are both shared begin in different CTAs, so c0 names the counter.)
+__device__ __forceinline__ bool arrives_last(unsigned* counter, int parts) {
+    __threadfence();
+    const bool last = atomicAdd(counter, 1u) == (unsigned)parts - 1u;
+    if (last) {
+        *counter = 0;
+        __threadfence();
+    }
+    return last;
+}
 
 // The pool as a rank-3 tensor (64 channels, rows of all pages, d / 64) in boxes of 64 channels x rows x chunks: a box lies in
 // shared memory as [chunk][row][128 bytes], swizzled.
 bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages, uint32_t rows, uint32_t chunks, CUtensorMap* map);
-// Joins what several CTAs left of a row tile.
-ea_status ea_launch_paged_combine(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, int rows, int BK, int ctas, cudaStream_t st);
 // Row tiles of 128 on the tensor cores (paged_chunk.cu).
 size_t ea_paged_chunk_ws_floats(int d);
 ea_status ea_launch_paged_chunk(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, const void* k_pages, const void* v_pages,
@@ -239,6 +241,8 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ float lse_of(float m, float l) {
     return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
+// 1 / l for a row's normalisation: zero for a row that sees no key, NaN stays
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }
 __device__ __forceinline__ float max3(float x, float y, float z) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));

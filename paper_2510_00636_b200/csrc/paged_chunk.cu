@@ -81,6 +81,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     auto drained = [&](int t) { return bars + 8u * (2 * NS + 14 + t); };      // only used when a wait has given up
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * C::BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
+    volatile int* last_flag = abort_flag + 1;           // per row tile: this CTA joins its parts
     Walk* start = reinterpret_cast<Walk*>(tail + C::TAIL_WALK);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
@@ -453,26 +454,80 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             uses[0] += (uint32_t)(count + 1) / 2;
             uses[1] += (uint32_t)count / 2;
             tc_fence_after_sync();
-            const bool whole = it.b0 == 0 && it.b1 == it.blocks;
-            const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-            if (whole) {
-                // through shared memory (where the queries were: every product with them has ended), so that rows leave
-                // in one piece
+            // Rows leave in one piece through shared memory (where the queries were: every product with them has ended).
+            auto stage = [&](int c, const float (&o)[32], float f) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8)
+                    sts128(q_place(row, (half * OWN + c + e) / 8),
+                           make_uint4(pack_bf16(o[e] * f, o[e + 1] * f), pack_bf16(o[e + 2] * f, o[e + 3] * f),
+                                      pack_bf16(o[e + 4] * f, o[e + 5] * f), pack_bf16(o[e + 6] * f, o[e + 7] * f)));
+            };
+            bool write = true;
+            if (it.b0 == 0 && it.b1 == it.blocks) {
+                const float inv = inverse_sum(l);
+#pragma unroll 1
+                for (int c = 0; c < OWN; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld_x32(o_col + c, o);
+                    tmem_ld_wait();
+                    float f[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(o[e]);
+                    stage(c, f, inv);
+                }
+            } else {
+                // a part: [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) write side by side
+                const Shared sh = shared_by(it, walk.total, gridDim.x);
+                const size_t own = (size_t)2 * blockIdx.x + (it.first ? 0 : 1);
+                float* part = a.part_o + (half * OWN * C::ROWS + (t * 128 + row) * 4);
+                float2* ml = reinterpret_cast<float2*>(a.part_ml) + t * 128 + row;
 #pragma unroll 1
                 for (int c = 0; c < OWN; c += 32) {
                     uint32_t o[32];
                     tmem_ld_x32(o_col + c, o);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 v;
-                        v.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                        v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-                        v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-                        v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                        sts128(q_place(row, (half * OWN + c + e) / 8), v);
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4*>(part + own * C::ROWS * D + (c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+                if (half == 0) ml[own * C::ROWS] = make_float2(m, l);
+                bar_sync(5 + t, TILE_THREADS);
+                if (tid == 0) last_flag[t] = arrives_last(a.counters + 2 * sh.c0 + t, sh.parts) ? 1 : 0;
+                bar_sync(5 + t, TILE_THREADS);
+                write = last_flag[t] != 0;
+                if (write) {
+                    m = -INFINITY;
+                    for (int p = 0; p < sh.parts; ++p) m = fmaxf(m, __ldcg(ml + (size_t)sh.slot(p) * C::ROWS).x);
+                    const float z = m == -INFINITY ? 0.f : m;
+                    l = 0.f;
+                    for (int p = 0; p < sh.parts; ++p) {
+                        const float2 v = __ldcg(ml + (size_t)sh.slot(p) * C::ROWS);
+                        l += v.y * ex2(v.x - z);
+                    }
+                    const float inv = inverse_sum(l);
+#pragma unroll 1
+                    for (int c = 0; c < OWN; c += 32) {
+                        float o[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+#pragma unroll 2
+                        for (int p = 0; p < sh.parts; ++p) {
+                            const size_t at = (size_t)sh.slot(p) * C::ROWS;
+                            const float w = ex2(__ldcg(ml + at).x - z);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 v = __ldcg(reinterpret_cast<const float4*>(part + at * D + (c + e) * C::ROWS));
+                                o[e] += v.x * w;
+                                o[e + 1] += v.y * w;
+                                o[e + 2] += v.z * w;
+                                o[e + 3] += v.w * w;
+                            }
+                        }
+                        stage(c, o, inv);
                     }
                 }
+            }
+            if (write) {
                 bar_sync(5 + t, TILE_THREADS);
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i) {
@@ -482,20 +537,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         *reinterpret_cast<uint4*>(a.out + ((size_t)(li.q0 + tk) * a.Hq + h) * D + piece * 8) = lds128(q_place(r, piece));
                 }
                 if (live && half == 0 && a.lse) a.lse[(size_t)(li.q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G] = lse_of(m, l);
-            } else {
-                // a part: [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) write side by side
-                const size_t slot = (size_t)2 * blockIdx.x + (it.first ? 0 : 1);
-                float* dst = a.part_o + slot * C::ROWS * D + (t * 128 + row) * 4;
-#pragma unroll 1
-                for (int c = 0; c < OWN; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld_x32(o_col + c, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4*>(dst + (half * OWN + c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                }
-                if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * C::ROWS + t * 128 + row) * 2) = make_float2(m, l);
             }
             __syncwarp();
             // (the loads above precede this pair's next exchange, and with it the weights that let the next item's
@@ -530,9 +571,7 @@ ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& arg
     if (err != EA_OK) return err;
     kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
     ea_count_launches(ctx, 1);
-    err = EA_CHECK_LAUNCH();
-    if (err != EA_OK) return err;
-    return ea_launch_paged_combine(ctx, s, a, C::ROWS, C::BK, ctas, st);
+    return EA_CHECK_LAUNCH();
 }
 
 }  // namespace
