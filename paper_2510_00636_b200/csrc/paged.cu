@@ -11,6 +11,7 @@
 // So the free list is either only read or only written, every entry of the table has one writer, and no order
 // between threads matters.  A shrink that undoes a growth leaves the free list as it was.
 #include "paged.h"
+#include "fast_div.cuh"
 #include "ptx_sm100.cuh"
 
 namespace {
@@ -30,8 +31,10 @@ struct PlanArgs {
     int32_t* slots;
     int32_t* offsets;
     int32_t* scratch;            // prefixes of more than kSelfScanLists lists, and the totals
+    unsigned* counter;           // arrivals of page_resize_kernel, zero between calls
     int* status;                 // [1]: page status word
     int lists, Hkv, shift, n_pages, max_pages, by_token, slot_capacity;
+    FastDiv div_hkv;             // by Hkv
 };
 
 // What a scan finds.  All-or-nothing: a call that cannot be served has n_take = n_give = rows = 0.
@@ -58,74 +61,68 @@ __device__ __forceinline__ void count_list(const PlanArgs& a, int r, Tally& t) {
     t.give += have > want ? have - want : 0;
     t.rows += n > o ? n - o : 0;
     // token order puts the heads of a token side by side: they must gain the same rows
-    if (a.by_token && r % a.Hkv != 0) {
-        const int o0 = a.old_lens[r - r % a.Hkv], n0 = a.new_lens[r - r % a.Hkv];
+    const int head0 = quotient(r, a.div_hkv) * a.Hkv;
+    if (a.by_token && r != head0) {
+        const int o0 = a.old_lens[head0], n0 = a.new_lens[head0];
         if ((n > o ? n - o : 0) != (n0 > o0 ? n0 - o0 : 0)) t.bad = 1;
     }
 }
-
-__device__ __forceinline__ long long shfl_up_ll(long long v, int d) { return __shfl_up_sync(0xffffffffu, v, d); }
 
 // Exclusive prefixes of pages taken, pages given back and rows gained, over all lists, into take / give / rows
 // (lists + 1 entries each; shared or global memory).  Every thread of the CTA calls it; the totals are returned
 // to all of them.  Entries hold 32 bits: totals beyond that are refused.
 template <int THREADS>
 __device__ Totals scan_lists(const PlanArgs& a, int32_t* take, int32_t* give, int32_t* rows) {
-    __shared__ Tally warp_sum[THREADS / 32];
+    constexpr int WARPS = THREADS / 32;
+    __shared__ long long sums[3][WARPS];
     __shared__ Totals total;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.lists + THREADS - 1) / THREADS;
     const int r0 = min(a.lists, tid * per), r1 = min(a.lists, r0 + per);
     Tally mine = {0, 0, 0, 0};
     for (int r = r0; r < r1; ++r) count_list(a, r, mine);
-    Tally inc = mine;
+    auto scan = [&](long long v) {                       // inclusive, over a warp
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long x = shfl_up_ll(inc.take, d), y = shfl_up_ll(inc.give, d), z = shfl_up_ll(inc.rows, d);
-        if (lane >= d) {
-            inc.take += x;
-            inc.give += y;
-            inc.rows += z;
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += x;
         }
+        return v;
+    };
+    const long long it = scan(mine.take), ig = scan(mine.give), ir = scan(mine.rows);
+    if (lane == 31) {
+        sums[0][warp] = it;
+        sums[1][warp] = ig;
+        sums[2][warp] = ir;
     }
-    const int any_bad = __any_sync(0xffffffffu, mine.bad);
-    if (lane == 31) warp_sum[warp] = {inc.take, inc.give, inc.rows, any_bad};
-    __syncthreads();
-    long long bt = 0, bg = 0, br = 0, tt = 0, tg = 0, tr = 0;
-    int bad = 0;
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w == warp) {
-            bt = tt;
-            bg = tg;
-            br = tr;
-        }
-        tt += warp_sum[w].take;
-        tg += warp_sum[w].give;
-        tr += warp_sum[w].rows;
-        bad |= warp_sum[w].bad;
+    int bad = __syncthreads_or(mine.bad);
+    // every warp scans the warps' sums
+    long long before[3], all[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const long long own = lane < WARPS ? sums[k][lane] : 0, inc = scan(own);
+        before[k] = __shfl_sync(0xffffffffu, inc - own, warp);
+        all[k] = __shfl_sync(0xffffffffu, inc, 31);
     }
     if (tid == 0) {
         int top = 0;
         if (a.free_pages) {
             top = *a.n_free;
-            if (top < 0 || top > a.n_pages || tt - tg > top || top + tg - tt > a.n_pages || tt > a.n_pages || tg > a.n_pages) bad = 1;
+            if (top < 0 || top > a.n_pages || all[0] - all[1] > top || top + all[1] - all[0] > a.n_pages || all[0] > a.n_pages || all[1] > a.n_pages)
+                bad = 1;
         }
-        if (tr > 0x7fffffffLL) bad = 1;
-        if (a.slots && tr > a.slot_capacity) bad = 1;
-        total = bad ? Totals{0, 0, 0, top, 1} : Totals{(int)tt, (int)tg, (int)tr, top, 0};
+        if (all[2] > 0x7fffffffLL) bad = 1;
+        if (a.slots && all[2] > a.slot_capacity) bad = 1;
+        total = bad ? Totals{0, 0, 0, top, 1} : Totals{(int)all[0], (int)all[1], (int)all[2], top, 0};
     }
     __syncthreads();
     const Totals out = total;
-    long long t = bt + inc.take - mine.take, g = bg + inc.give - mine.give, n = br + inc.rows - mine.rows;
+    Tally at = {before[0] + it - mine.take, before[1] + ig - mine.give, before[2] + ir - mine.rows, 0};
     for (int r = r0; r < r1; ++r) {
-        take[r] = out.bad ? 0 : (int)t;
-        give[r] = out.bad ? 0 : (int)g;
-        rows[r] = out.bad ? 0 : (int)n;
-        Tally one = {0, 0, 0, 0};
-        count_list(a, r, one);
-        t += one.take;
-        g += one.give;
-        n += one.rows;
+        take[r] = out.bad ? 0 : (int)at.take;
+        give[r] = out.bad ? 0 : (int)at.give;
+        rows[r] = out.bad ? 0 : (int)at.rows;
+        if (r + 1 < r1) count_list(a, r, at);
     }
     if (tid == 0) {
         take[a.lists] = out.n_take;
@@ -175,46 +172,47 @@ __device__ __forceinline__ int slot_of(const PlanArgs& a, int r, int p) {
     return (unsigned)page < (unsigned)a.n_pages ? (page << a.shift) + (p & ((1 << a.shift) - 1)) : -1;
 }
 
-// Slots 4 t .. 4 t + 3 for t = t0, t0 + step, ...: rows old .. new of every list, -1 behind the last.
-__device__ void write_slots(const PlanArgs& a, const Totals& tot, const int32_t* rows, long long t0, long long step) {
-    const bool wide = (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
-    for (long long q = t0; q * 4 < a.slot_capacity; q += step) {
-        int v[4];
-        int r = -1, next = 0;                                        // list order: the list of the last slot, and where it ends
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const long long t = q * 4 + e;
-            v[e] = -1;
-            if (t >= tot.rows) continue;
-            if (a.by_token) {
-                // rows[] counts Hkv rows per token: token t / Hkv begins its sequence at rows[s * Hkv] / Hkv
-                const int token = (int)(t / a.Hkv), g = (int)(t % a.Hkv);
-                const int s = find_list(rows, a.lists, token * a.Hkv) / a.Hkv;      // lists of a sequence gain alike
-                const int list = s * a.Hkv + g;
-                v[e] = slot_of(a, list, a.old_lens[list] + token - rows[s * a.Hkv] / a.Hkv);
-            } else {
-                if (r < 0 || t >= next) {
-                    r = find_list(rows, a.lists, (int)t);
-                    next = rows[r + 1];
-                }
-                v[e] = slot_of(a, r, a.old_lens[r] + (int)t - rows[r]);
-            }
-        }
-        if (wide && q * 4 + 4 <= a.slot_capacity) {
-            reinterpret_cast<int4*>(a.slots)[q] = make_int4(v[0], v[1], v[2], v[3]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (q * 4 + e < a.slot_capacity) a.slots[q * 4 + e] = v[e];
-        }
+// The slot of new row t of the call (rows old .. new of every list), -1 behind the last.  `r`, `next`: in list order, the
+// list of the thread's slot before and where it ends.
+__device__ __forceinline__ int slot_at(const PlanArgs& a, const Totals& tot, const int32_t* rows, long long t, int& r, int& next) {
+    if (t >= tot.rows) return -1;
+    if (a.by_token) {
+        // rows[] counts Hkv rows per token: token t / Hkv begins its sequence at rows[s * Hkv] / Hkv
+        const int token = quotient((int)t, a.div_hkv), g = (int)t - token * a.Hkv;
+        const int s = quotient(find_list(rows, a.lists, token * a.Hkv), a.div_hkv);      // lists of a sequence gain alike
+        const int list = s * a.Hkv + g;
+        return slot_of(a, list, a.old_lens[list] + token - quotient(rows[s * a.Hkv], a.div_hkv));
     }
+    if (r < 0 || t >= next) {
+        r = find_list(rows, a.lists, (int)t);
+        next = rows[r + 1];
+    }
+    return slot_of(a, r, a.old_lens[r] + (int)t - rows[r]);
+}
+
+// The CTA's share of the slots, side by side, so that a thread mostly stays in the list of its slot before: one at a time
+// where they are few (the chain of dependent loads is the time), four where they are many.
+__device__ void write_slots(const PlanArgs& a, const Totals& tot, const int32_t* rows) {
+    int r = -1, next = 0;
+    const bool wide = a.slot_capacity > (long long)gridDim.x * blockDim.x && (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0;
+    const long long quads = wide ? a.slot_capacity / 4 : 0;
+    const long long share = (quads + gridDim.x - 1) / gridDim.x, end = min(quads, (blockIdx.x + 1) * share);
+    for (long long q = blockIdx.x * share + threadIdx.x; q < end; q += blockDim.x) {
+        int v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = slot_at(a, tot, rows, q * 4 + e, r, next);
+        reinterpret_cast<int4*>(a.slots)[q] = make_int4(v[0], v[1], v[2], v[3]);
+    }
+    r = -1;
+    for (long long t = quads * 4 + (long long)blockIdx.x * blockDim.x + threadIdx.x; t < a.slot_capacity; t += (long long)gridDim.x * blockDim.x)
+        a.slots[t] = slot_at(a, tot, rows, t, r, next);
 }
 
 // Offsets (list order: lists + 1 row offsets; token order: sequences + 1 token offsets), the free count, the status.
 __device__ void write_offsets(const PlanArgs& a, const Totals& tot, const int32_t* rows) {
     if (a.offsets) {
         const int n = a.by_token ? a.lists / a.Hkv : a.lists;
-        for (int i = threadIdx.x; i <= n; i += blockDim.x) a.offsets[i] = a.by_token ? rows[i * a.Hkv] / a.Hkv : rows[i];
+        for (int i = threadIdx.x; i <= n; i += blockDim.x) a.offsets[i] = a.by_token ? quotient(rows[i * a.Hkv], a.div_hkv) : rows[i];
     }
     if (threadIdx.x == 0) {
         if (a.free_pages && !tot.bad) *a.n_free = tot.top - tot.n_take + tot.n_give;
@@ -235,8 +233,22 @@ __global__ void __launch_bounds__(kScanThreads) page_plan_cluster_kernel(const P
         move_pages(a, tot, take, give, t0, step);
         ptx::cluster_sync();                                        // the slots read the entries just written
     }
-    if (a.slots) write_slots(a, tot, rows, t0, step);
+    if (a.slots) write_slots(a, tot, rows);
     if (blockIdx.x == 0) write_offsets(a, tot, rows);
+}
+
+// A plan without slots over all SMs in one launch: every CTA scans the lengths for itself and moves its share of the
+// pages; the free count is written by the CTA that arrives last, when all others have read it.
+__global__ void __launch_bounds__(kMoveThreads) page_resize_kernel(const PlanArgs a) {
+    extern __shared__ int32_t prefix[];
+    __shared__ bool last;
+    int32_t *take = prefix, *give = take + a.lists + 1, *rows = give + a.lists + 1;
+    const Totals tot = scan_lists<kMoveThreads>(a, take, give, rows);
+    move_pages(a, tot, take, give, blockIdx.x * kMoveThreads + threadIdx.x, gridDim.x * kMoveThreads);
+    __syncthreads();
+    if (threadIdx.x == 0) last = arrives_last(a.counter, gridDim.x);
+    __syncthreads();
+    if (last) write_offsets(a, tot, rows);
 }
 
 // Larger plans: prefixes and totals into the workspace, then the pages, then the slots.
@@ -267,7 +279,7 @@ __global__ void __launch_bounds__(kMoveThreads) page_slots_kernel(const PlanArgs
         rows = a.scratch + 2 * (a.lists + 1);
         tot = *reinterpret_cast<const Totals*>(rows + a.lists + 1);
     }
-    if (a.slots) write_slots(a, tot, rows, (long long)blockIdx.x * kMoveThreads + threadIdx.x, (long long)gridDim.x * kMoveThreads);
+    if (a.slots) write_slots(a, tot, rows);
 }
 
 // rows <-> slots, 16 bytes of K and of V per thread and step.  A slot of -1 names no row; any other number outside the
@@ -342,12 +354,21 @@ ea_status launch_plan(const ea_ctx* ctx, PlanArgs a, cudaStream_t st) {
         ea_count_launches(ctx, 1);
         return EA_CHECK_LAUNCH();
     }
+    if (few && !a.slots) {
+        // nothing bounds the pages that move but the pool
+        static std::atomic<uint64_t> done{0};
+        const ea_status err = ea_allow_smem(page_resize_kernel, kScanSmem, ctx->device, done);
+        if (err != EA_OK) return err;
+        const long long ctas = ((long long)a.n_pages + 4 * kMoveThreads - 1) / (4 * kMoveThreads), most = ctx->sm_count;
+        page_resize_kernel<<<(unsigned)(ctas < 1 ? 1 : ctas < most ? ctas : most), kMoveThreads, smem, st>>>(a);
+        ea_count_launches(ctx, 1);
+        return EA_CHECK_LAUNCH();
+    }
     if (few && a.slot_capacity <= kClusterSlots) {
         static std::atomic<uint64_t> done{0};
         const ea_status err = ea_allow_smem(page_plan_cluster_kernel, kScanSmem, ctx->device, done);
         if (err != EA_OK) return err;
-        // without slots nothing bounds the pages that move but the pool, so that form gets the wide cluster
-        const unsigned ctas = a.slots && a.slot_capacity <= kOneCtaSlots ? 1 : 8;
+        const unsigned ctas = a.slot_capacity <= kOneCtaSlots ? 1 : 8;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(ctas);
         cfg.blockDim = dim3(kScanThreads);
@@ -400,8 +421,10 @@ ea_status plan_call(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old
     a.offsets = offsets;
     a.scratch = static_cast<int32_t*>(ctx->workspace);
     a.status = ctx->status_dev;
+    a.counter = ctx->counters + kCounters - 1;
     a.lists = (int)lists;
     a.Hkv = shape->n_kv_heads;
+    a.div_hkv = fast_div(a.Hkv);
     a.shift = __builtin_ctz((unsigned)shape->page_rows);
     a.n_pages = shape->n_pages;
     a.max_pages = shape->max_pages;

@@ -5,6 +5,18 @@
 
 #include "ea_internal.h"
 
+// Called by one thread of each of `parts` CTAs, once the threads that wrote have met at a barrier: whether the others have all
+// been here (and what they wrote can be read).  The last one puts the counter back to zero.
+__device__ __forceinline__ bool arrives_last(unsigned* counter, int parts) {
+    __threadfence();
+    const bool last = atomicAdd(counter, 1u) == (unsigned)parts - 1u;
+    if (last) {
+        *counter = 0;
+        __threadfence();
+    }
+    return last;
+}
+
 // Lets a kernel use more than 48 KiB of dynamic shared memory: once per device (a runtime call that a generation step
 // would otherwise pay at each layer); `done` belongs to the kernel.
 template <class Kernel>

@@ -47,7 +47,7 @@ template <int D> struct Few {
 // weights (in `weight`, [16][parts]), then every thread adds 4 channels of a row over the parts.
 template <int D, int THREADS>
 __device__ void join_parts(const AttnArgs& a, const Shared& sh, float* weight, int live, int row0, int q0, int head0) {
-    constexpr int LANES = THREADS / 16;
+    constexpr int LANES = THREADS / 16, BATCH = D == 256 ? 8 : 16;
     {
         const int row = threadIdx.x / LANES, lane = threadIdx.x % LANES;
         float m = -INFINITY, l = 0.f;
@@ -82,15 +82,15 @@ __device__ void join_parts(const AttnArgs& a, const Shared& sh, float* weight, i
         if (row >= live) continue;
         const float* src = a.part_o + (col * 16) + row * 4;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int b = 0; b < sh.parts; b += 8) {          // eight loads on their way at a time
-            float4 v[8];
+        for (int b = 0; b < sh.parts; b += BATCH) {      // so many loads on their way at a time
+            float4 v[BATCH];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < BATCH; ++k) {
                 v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (b + k < sh.parts) v[k] = __ldcg(reinterpret_cast<const float4*>(src + (size_t)sh.slot(b + k) * 16 * D));
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < BATCH; ++k) {
                 const float w = b + k < sh.parts ? weight[row * kPagedMaxCtas + b + k] : 0.f;
                 o.x += v[k].x * w;
                 o.y += v[k].y * w;
@@ -348,24 +348,33 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     o[i][2 * x + 1] *= f;
                 }
             }
+            const bool upper = li.rows_tok * a.G - tile * 16 > 8;       // rows 8-15 of the tile are in use
 #pragma unroll
             for (int h = C::NW / 2; h >= 1; h /= 2) {
                 if (warp >= h && warp < 2 * h) {
-                    float4* dst = reinterpret_cast<float4*>(merge) + (size_t)(h == C::NW / 2 ? warp - h : warp) * (D / 8) * 32 + lane;
+                    float2* dst = reinterpret_cast<float2*>(merge) + (size_t)(h == C::NW / 2 ? warp - h : warp) * (D / 8) * 64 + lane;
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) dst[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+                    for (int i = 0; i < D / 8; ++i) dst[i * 64] = make_float2(o[i][0], o[i][1]);
+                    if (upper)
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) dst[i * 64 + 32] = make_float2(o[i][2], o[i][3]);
                 }
                 bar_sync(1, C::NW * 32);
                 if (warp < h) {
-                    const float4* src = reinterpret_cast<const float4*>(merge) + (size_t)(h == C::NW / 2 ? warp : warp + h) * (D / 8) * 32 + lane;
+                    const float2* src = reinterpret_cast<const float2*>(merge) + (size_t)(h == C::NW / 2 ? warp : warp + h) * (D / 8) * 64 + lane;
 #pragma unroll
                     for (int i = 0; i < D / 8; ++i) {
-                        const float4 v = src[i * 32];
+                        const float2 v = src[i * 64];
                         o[i][0] += v.x;
                         o[i][1] += v.y;
-                        o[i][2] += v.z;
-                        o[i][3] += v.w;
                     }
+                    if (upper)
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) {
+                            const float2 v = src[i * 64 + 32];
+                            o[i][2] += v.x;
+                            o[i][3] += v.y;
+                        }
                 }
             }
             const bool whole = b0 == 0 && it.b1 == it.blocks;

@@ -5,19 +5,8 @@
 #include <cuda_bf16.h>
 
 #include "ea_internal.h"
-
-// Division of 0 <= n < 2^31 by a fixed d >= 1 without a divide: with l = ceil(log2 d) and mul = ceil(2^(31 + l) / d) < 2^32,
-// mul d exceeds 2^(31 + l) by less than 2^l, so that n mul / 2^(31 + l) is off by less than 1 / d.
-struct FastDiv {
-    uint32_t mul;
-    int shift, d;
-};
-static inline FastDiv fast_div(int d) {
-    int l = 0;
-    while ((1 << l) < d) ++l;
-    return {d == 1 ? 0u : (uint32_t)(((1ull << (31 + l)) + (uint32_t)d - 1) / (uint32_t)d), l - 1, d};
-}
-__device__ __forceinline__ int quotient(int n, const FastDiv& f) { return f.shift < 0 ? n : (int)(__umulhi((uint32_t)n, f.mul) >> f.shift); }
+#include "fast_div.cuh"
+#include "paged.h"
 
 struct AttnArgs {
     const __nv_bfloat16* q;
@@ -197,7 +186,8 @@ static_assert(2 * kPagedMaxCtas <= kCounters, "a counter per CTA and row tile");
 
 // The CTAs that share a row tile: `parts` of them from c0 on.  Each leaves its part (maxima, sums, unnormalised output)
 // in a slot of the workspace, and the one that arrives last joins them, in the order of the keys.  A CTA's first item
-// is its slot 0, its last slot 1; only the tile's first CTA may have begun before the tile.
+// is its slot 0, its last slot 1; only the tile's first CTA may have begun before the tile.  (Two tiles that are both
+// shared begin in different CTAs, so c0 names the counter of the arrivals.)
 struct Shared {
     int c0, parts, first_slot;
     __device__ __forceinline__ int slot(int p) const { return p == 0 ? first_slot : 2 * (c0 + p); }
@@ -210,17 +200,6 @@ __device__ __forceinline__ Shared shared_by(const Item& it, long long total, int
     s.parts = d.owner(u0 + it.blocks - 1) - s.c0 + 1;
     s.first_slot = 2 * s.c0 + (u0 > d.begin(s.c0) ? 1 : 0);
     return s;
-}
-// Called by one thread once the part's writers have met at a barrier: whether the other parts are all there.  (Two tiles
-// that are both shared begin in different CTAs, so c0 names the counter.)
-__device__ __forceinline__ bool arrives_last(unsigned* counter, int parts) {
-    __threadfence();
-    const bool last = atomicAdd(counter, 1u) == (unsigned)parts - 1u;
-    if (last) {
-        *counter = 0;
-        __threadfence();
-    }
-    return last;
 }
 
 // The pool as a rank-3 tensor (64 channels, rows of all pages, d / 64) in boxes of 64 channels x rows x chunks: a box lies in
