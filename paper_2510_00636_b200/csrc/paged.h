@@ -17,6 +17,16 @@ __device__ __forceinline__ bool arrives_last(unsigned* counter, int parts) {
     return last;
 }
 
+// Whether all others have arrived already (then the caller is the last, and the counter is put back to zero).
+__device__ __forceinline__ bool others_arrived(unsigned* counter, int parts) {
+    const bool last = *reinterpret_cast<volatile unsigned*>(counter) == (unsigned)parts - 1u;
+    if (last) {
+        __threadfence();
+        *counter = 0;
+    }
+    return last;
+}
+
 // Lets a kernel use more than 48 KiB of dynamic shared memory: once per device (a runtime call that a generation step
 // would otherwise pay at each layer); `done` belongs to the kernel.
 template <class Kernel>

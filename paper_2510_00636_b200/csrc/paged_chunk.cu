@@ -478,30 +478,37 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             } else {
                 // a part: [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) write side by side
                 const Shared sh = shared_by(it, walk.total, gridDim.x);
-                const size_t own = (size_t)2 * blockIdx.x + (it.first ? 0 : 1);
+                const int own = 2 * (int)blockIdx.x + (it.first ? 0 : 1);
                 float* part = a.part_o + (half * OWN * C::ROWS + (t * 128 + row) * 4);
                 float2* ml = reinterpret_cast<float2*>(a.part_ml) + t * 128 + row;
-#pragma unroll 1
-                for (int c = 0; c < OWN; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld_x32(o_col + c, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4*>(part + own * C::ROWS * D + (c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                }
-                if (half == 0) ml[own * C::ROWS] = make_float2(m, l);
-                bar_sync(5 + t, TILE_THREADS);
-                if (tid == 0) last_flag[t] = arrives_last(a.counters + 2 * sh.c0 + t, sh.parts) ? 1 : 0;
+                // if all others have arrived, this part need not be written
+                if (tid == 0) last_flag[t] = others_arrived(a.counters + 2 * sh.c0 + t, sh.parts) ? 1 : 0;
                 bar_sync(5 + t, TILE_THREADS);
                 write = last_flag[t] != 0;
+                if (!write) {
+#pragma unroll 1
+                    for (int c = 0; c < OWN; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld_x32(o_col + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<uint4*>(part + (size_t)own * C::ROWS * D + (c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
+                    if (half == 0) ml[(size_t)own * C::ROWS] = make_float2(m, l);
+                    bar_sync(5 + t, TILE_THREADS);
+                    if (tid == 0) last_flag[t] = arrives_last(a.counters + 2 * sh.c0 + t, sh.parts) ? 1 : 0;
+                    bar_sync(5 + t, TILE_THREADS);
+                    write = last_flag[t] != 0;
+                }
                 if (write) {
-                    m = -INFINITY;
-                    for (int p = 0; p < sh.parts; ++p) m = fmaxf(m, __ldcg(ml + (size_t)sh.slot(p) * C::ROWS).x);
+                    const float m_own = m, l_own = l;
+                    auto stats_of = [&](int p) { return sh.slot(p) == own ? make_float2(m_own, l_own) : __ldcg(ml + (size_t)sh.slot(p) * C::ROWS); };
+                    for (int p = 0; p < sh.parts; ++p) m = fmaxf(m, stats_of(p).x);
                     const float z = m == -INFINITY ? 0.f : m;
                     l = 0.f;
                     for (int p = 0; p < sh.parts; ++p) {
-                        const float2 v = __ldcg(ml + (size_t)sh.slot(p) * C::ROWS);
+                        const float2 v = stats_of(p);
                         l += v.y * ex2(v.x - z);
                     }
                     const float inv = inverse_sum(l);
@@ -510,17 +517,27 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                         float o[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0.f;
-#pragma unroll 2
-                        for (int p = 0; p < sh.parts; ++p) {
-                            const size_t at = (size_t)sh.slot(p) * C::ROWS;
-                            const float w = ex2(__ldcg(ml + at).x - z);
+#pragma unroll 1
+                        for (int p = 0; p < sh.parts; ++p) {       // in the order of the keys, this CTA's own from where it is
+                            const float w = ex2(stats_of(p).x - z);
+                            if (sh.slot(p) == own) {
+                                uint32_t v[32];
+                                tmem_ld_x32(o_col + c, v);
+                                tmem_ld_wait();
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 v = __ldcg(reinterpret_cast<const float4*>(part + at * D + (c + e) * C::ROWS));
-                                o[e] += v.x * w;
-                                o[e + 1] += v.y * w;
-                                o[e + 2] += v.z * w;
-                                o[e + 3] += v.w * w;
+                                for (int e = 0; e < 32; ++e) o[e] += __uint_as_float(v[e]) * w;
+                            } else {
+                                const float* src = part + (size_t)sh.slot(p) * C::ROWS * D + c * C::ROWS;
+                                float4 v[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] = __ldcg(reinterpret_cast<const float4*>(src + e * 4 * C::ROWS));
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    o[4 * e] += v[e].x * w;
+                                    o[4 * e + 1] += v[e].y * w;
+                                    o[4 * e + 2] += v[e].z * w;
+                                    o[4 * e + 3] += v[e].w * w;
+                                }
                             }
                         }
                         stage(c, o, inv);
