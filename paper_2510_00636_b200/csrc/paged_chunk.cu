@@ -5,7 +5,7 @@
 //     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
 //     P = 2^(c S - m)  running maximum m and sum l per row; P (bf16) in tensor memory, two buffers per tile
 //     O += P V         A = P from tensor memory, B = V as it lies (rows are the contraction index: MN-major)
-// One warp keeps K and V flowing through a ring of slots (TMA boxes of a page each), one warp per row tile issues its MMAs
+// Two warps keep K and V flowing through a ring of slots each (TMA boxes of a page), one warp per row tile issues its MMAs
 // (the waits of one are hidden by the other's), eight warps do the softmax, 64 scores per thread and block.  The scores of
 // the next block are on their way as soon as those of this one have been read.
 //
@@ -13,6 +13,8 @@
 // bf16 range, and the sum, which uses the same maximum, cancels it): O is rescaled in tensor memory only then.
 //
 // The CTAs divide the call's (row tile, key block) units evenly, as in the kernel for few rows (paged_attn.cuh).
+#include <type_traits>
+
 #include "paged.h"
 #include "paged_attn.cuh"
 #include "ptx_sm100.cuh"
@@ -28,14 +30,13 @@ template <int D> struct Chunk {
     static constexpr int HALVES = 2 / TILES;            // threads per row (each has 64 keys of a block)
     static constexpr int ROWS = TILES * 128;
     static constexpr int BK = HALVES * 64;              // keys per block
-    // a slot of the ring: K: all keys of a block x KW * 64 channels;  V: VKEYS keys x all channels
+    // a slot of its ring: K: all keys of a block x KW * 64 channels;  V: VKEYS keys x all channels
     static constexpr uint32_t SLOT = D == 64 ? 8192 : 16384;
     static constexpr int KW = (int)SLOT / (BK * 128), KC = D / 64 / KW;
     static constexpr int VKEYS = (int)SLOT / (D * 2), VC = BK / VKEYS;
-    static constexpr int PER_BLOCK = KC + VC;
     static constexpr uint32_t Q_TILE = 128u * D * 2;
-    static constexpr int NSLOT = D == 64 ? 20 : D == 128 ? 10 : 9;
-    static constexpr int THREADS = 128 + 256;           // warps 0 (loads), 1 and 2 (MMA of a row tile), an idle one, the softmax warps
+    static constexpr int NSLOT = D == 64 ? 20 : D == 128 ? 10 : 9, NV = NSLOT / 2, NK = NSLOT - NV;   // K's ring, then V's
+    static constexpr int THREADS = 128 + 256;           // warps 0 and 3 (K, V), 1 and 2 (MMA of a row tile), then the softmax warps
     static constexpr int BARS = 2 * NSLOT + 16;
     static constexpr int TAIL_WALK = BARS * 8 + 16;
     static constexpr int TAIL_STATS = TAIL_WALK + (int)sizeof(Walk);
@@ -44,16 +45,14 @@ template <int D> struct Chunk {
     static constexpr uint32_t O_COL = 256;              // tensor memory: S of tile t at 2 t BK, P of buffer b BK + b BK / 2 on, O from 256
     static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
     static_assert(KC * KW * 64 == D && VC * VKEYS == BK && VKEYS % 16 == 0, "slots");
-    // Order of the blocks in the ring: K0 K1 V0 K2 V1 ...; where block j's V begins, in slots after the item's first
-    static __device__ __forceinline__ int v_at(int j, int count) { return (j + 2 < count ? j + 2 : count) * KC + j * VC; }
 };
 
 // A place in the ring: slot, and the parity of its use.
 struct Ring {
     uint32_t slot, phase;
-    __device__ __forceinline__ void next(int nslot) {
-        if (++slot == (uint32_t)nslot) {
-            slot = 0;
+    __device__ __forceinline__ void next(int first, int end) {
+        if (++slot == (uint32_t)end) {
+            slot = (uint32_t)first;
             phase ^= 1;
         }
     }
@@ -118,13 +117,17 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     Item it;
     bool ok = true;
 
-    if (warp == 0) {
-        // ------------------------------------------------------------------------------ K and V
-        Ring ring = {0, 0};
+    // ---------------------------------------------------------------------------------- K (warp 0) or V (warp 3)
+    auto feed = [&](auto is_v) {
+        constexpr bool V = decltype(is_v)::value;
+        // a slot: ROWS keys and WIDE times 64 channels; CHUNKS of them a block
+        constexpr int ROWS = V ? C::VKEYS : BK, WIDE = V ? D / 64 : C::KW, CHUNKS = V ? C::VC : C::KC;
+        constexpr int FIRST = V ? C::NK : 0, END = V ? NS : C::NK, MAX_SHIFT = ROWS == 128 ? 7 : ROWS == 64 ? 6 : 5;
         const uint32_t leader = elect_one();
-        const int kbox = min(1 << a.shift, BK), vbox = min(1 << a.shift, C::VKEYS);
+        const int box_shift = min(a.shift, MAX_SHIFT), row_mask = (1 << a.shift) - 1;      // keys of a box
+        Ring ring = {FIRST, 0};
         while (next_item(a, walk, C::ROWS, BK, it)) {
-            const int n = it.li.n, count = it.b1 - it.b0;
+            const int n = it.li.n;
             const int entries = (int)(((unsigned)n + (1u << a.shift) - 1u) >> a.shift);
             const int32_t* tab = a.table + (size_t)it.list * a.max_pages;
             auto entry = [&](int e) {
@@ -138,57 +141,52 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 }
                 return page;
             };
-            // table entries ride in registers: 32 from `win`, 32 after them (the next K block may lie there), 32 ahead
+            // table entries ride in registers, 32 ahead of the 32 in use
             int win = (int)(((long long)it.b0 * BK) >> a.shift) & ~31;
-            int e0 = entry(win + lane), e1 = entry(win + 32 + lane), e2 = entry(win + 64 + lane);
-            // block by block: K of block j + 1, then V of block j
-            for (int j = -1; j < count; ++j) {
-                const int at = (int)(((long long)(it.b0 + max(j, 0)) * BK) >> a.shift);
-                if (at >= win + 32) {
+            int cur = entry(win + lane), next = entry(win + 32 + lane);
+            for (int b = it.b0; b < it.b1; ++b) {
+                if (((b * BK) >> a.shift) >= win + 32) {
                     win += 32;
-                    e0 = e1;
-                    e1 = e2;
-                    e2 = entry(win + 64 + lane);
+                    cur = next;
+                    next = entry(win + 32 + lane);
                 }
-#pragma unroll 1
-                for (int i = 0; i < C::PER_BLOCK; ++i) {
-                    const bool is_v = i >= C::KC;
-                    const int jj = is_v ? j : j + 1, c = is_v ? i - C::KC : i;
-                    if (jj < 0 || jj >= count) continue;
-                    // `rows` keys from key0 and `wide` times 64 channels into one slot, in boxes of `box` keys
-                    const int key0 = (it.b0 + jj) * BK + (is_v ? c * C::VKEYS : 0);
-                    const int rows = is_v ? C::VKEYS : BK, box = is_v ? vbox : kbox, wide = is_v ? D / 64 : C::KW;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    const int key0 = b * BK + (V ? c * ROWS : 0), rest = n - key0;
+                    const int boxes = rest <= 0 ? 0 : min(ROWS >> box_shift, (rest + (1 << box_shift) - 1) >> box_shift);
                     if (ok) ok = mbar_wait(empty(ring.slot), ring.phase ^ 1, abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) continue;
-                    const int rest = n - key0;
-                    const int act = rest <= 0 ? 0 : rest >= rows ? rows / box : (rest + box - 1) / box;
-                    if (leader) mbar_arrive_expect_tx(full(ring.slot), (uint32_t)(act * box * 128 * wide));
                     __syncwarp();
-                    const uint32_t to = s_ring + ring.slot * C::SLOT;
-#pragma unroll 1
-                    for (int sub = 0; sub < act; ++sub) {
-                        const int key = key0 + sub * box, e = (key >> a.shift) - win;
-                        const int p0 = __shfl_sync(0xffffffffu, e0, e & 31), p1 = __shfl_sync(0xffffffffu, e1, e & 31);
-                        const int y = ((e < 32 ? p0 : p1) << a.shift) + (key & ((1 << a.shift) - 1));
-                        if (is_v) {                     // box after box: [64 channels][row][128 bytes] each
-                            tma_load_3d_warp(leader, to + (uint32_t)(sub * box) * (D * 2), &v_map, full(ring.slot), 0, y, 0);
+                    const uint32_t go = ok ? leader : 0u;
+                    const uint32_t bar = full(ring.slot), to = s_ring + ring.slot * C::SLOT;
+                    if (go) mbar_arrive_expect_tx(bar, (uint32_t)((boxes * 128 * WIDE) << box_shift));
+#pragma unroll 2
+                    for (int x = 0; x < boxes; ++x) {
+                        const int key = key0 + (x << box_shift);
+                        const int y = (__shfl_sync(0xffffffffu, cur, ((key >> a.shift) - win) & 31) << a.shift) + (key & row_mask);
+                        if (V) {                        // box after box: [64 channels][row][128 bytes] each
+                            tma_load_3d_warp(go, to + ((uint32_t)(x * D * 2) << box_shift), &v_map, bar, 0, y, 0);
                         } else {                        // the rows of a chunk of 64 channels side by side
 #pragma unroll
-                            for (int w = 0; w < C::KW; ++w)
-                                tma_load_3d_warp(leader, to + w * BK * 128 + (uint32_t)(sub * box) * 128u, &k_map, full(ring.slot), 0, y, c * C::KW + w);
+                            for (int w = 0; w < WIDE; ++w)
+                                tma_load_3d_warp(go, to + w * BK * 128 + ((uint32_t)(x * 128) << box_shift), &k_map, bar, 0, y, c * WIDE + w);
                         }
                     }
-                    ring.next(NS);
+                    ring.next(FIRST, END);
                 }
             }
         }
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok && lane == 0)
-            for (int s = 0; s < NS; ++s) {              // copies in flight land before the shared memory goes away
+            for (int s = FIRST; s < END; ++s) {         // copies in flight land before the shared memory goes away
                 mbar_drain(full(s), 0);
                 mbar_drain(full(s), 1);
             }
         __syncwarp();
+    };
+    if (warp == 0) {
+        feed(std::false_type());
+    } else if (warp == 3) {
+        feed(std::true_type());
     } else if (warp <= C::TILES) {
         // ------------------------------------------------------------------------------ MMA issuer of a row tile
         // The whole warp runs this loop in step, and one lane issues (see umma_bf16_warp).
@@ -205,16 +203,23 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             v_step[ks] = (uint32_t)__shfl_sync(0xffffffffu, ((ks * 16 >> vbits) * vbox * (D * 2 - 128) + ks * 2048) >> 4, 0);
         const uint32_t s_tmem = tmem + 2 * t * BK, o_tmem = tmem + C::O_COL + t * D;
         uint32_t p_phase = 0, q_phase = 0, r_phase = 0; // parity of the next phase of p_full(t, b) (bit b), q_full, s_read
-        Ring ring = {0, 0};
+        Ring k_ring = {0, 0}, v_ring = {(uint32_t)C::NK, 0};
         while (next_item(a, walk, C::ROWS, BK, it)) {
             const int count = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
             const int nt = __shfl_sync(0xffffffffu, C::TILES == 2 && it.li.rows_tok * a.G - it.tile * C::ROWS > 128 ? 2 : 1, 0);
             if (t >= nt) {                              // nothing to do with these blocks but to give their slots back
 #pragma unroll 1
-                for (int i = 0; i < count * C::PER_BLOCK; ++i) {
-                    if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
-                    if (leader) mbar_arrive(empty(ring.slot));
-                    ring.next(NS);
+                for (int i = 0; i < count; ++i) {
+                    for (int c = 0; c < C::KC; ++c) {
+                        if (ok) ok = mbar_wait(full(k_ring.slot), k_ring.phase, abort_flag);
+                        if (leader) mbar_arrive(empty(k_ring.slot));
+                        k_ring.next(0, C::NK);
+                    }
+                    for (int c = 0; c < C::VC; ++c) {
+                        if (ok) ok = mbar_wait(full(v_ring.slot), v_ring.phase, abort_flag);
+                        if (leader) mbar_arrive(empty(v_ring.slot));
+                        v_ring.next(C::NK, NS);
+                    }
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 continue;
@@ -230,18 +235,18 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     }
 #pragma unroll
                     for (int c = 0; c < C::KC; ++c) {
-                        if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
+                        if (ok) ok = mbar_wait(full(k_ring.slot), k_ring.phase, abort_flag);
                         ok = __all_sync(0xffffffffu, ok);
                         if (ok) {
                             tc_fence_after_sync();
-                            const uint64_t qd = q_desc + c * C::KW * (16384 >> 4), kd = k_desc + ring.slot * (C::SLOT >> 4);
+                            const uint64_t qd = q_desc + c * C::KW * (16384 >> 4), kd = k_desc + k_ring.slot * (C::SLOT >> 4);
 #pragma unroll
                             for (int ks = 0; ks < 4 * C::KW; ++ks)
                                 umma_bf16_warp(leader, s_tmem, qd + (ks / 4) * (16384 >> 4) + ks % 4 * 2, kd + (ks / 4) * (BK * 128 >> 4) + ks % 4 * 2,
                                                idesc_s, c + ks > 0 ? 1u : 0u);
-                            umma_commit_warp(leader, empty(ring.slot));
+                            umma_commit_warp(leader, empty(k_ring.slot));
                         }
-                        ring.next(NS);
+                        k_ring.next(0, C::NK);
                     }
                     if (ok) umma_commit_warp(leader, s_full(t));
                 }
@@ -251,18 +256,18 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     p_phase ^= 1u << b;
 #pragma unroll
                     for (int c = 0; c < C::VC; ++c) {
-                        if (ok) ok = mbar_wait(full(ring.slot), ring.phase, abort_flag);
+                        if (ok) ok = mbar_wait(full(v_ring.slot), v_ring.phase, abort_flag);
                         ok = __all_sync(0xffffffffu, ok);
                         if (ok) {
                             tc_fence_after_sync();
-                            const uint64_t vd = v_desc + ring.slot * (C::SLOT >> 4);
+                            const uint64_t vd = v_desc + v_ring.slot * (C::SLOT >> 4);
                             const uint32_t p_tmem = s_tmem + BK + b * (BK / 2) + c * (C::VKEYS / 2);
 #pragma unroll
                             for (int ks = 0; ks < C::VKEYS / 16; ++ks)
                                 umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
-                            umma_commit_warp(leader, empty(ring.slot));
+                            umma_commit_warp(leader, empty(v_ring.slot));
                         }
-                        ring.next(NS);
+                        v_ring.next(C::NK, NS);
                     }
                     if (ok) umma_commit_warp(leader, o_done(t, b));
                 }
@@ -287,7 +292,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS);
         const int vbox = min(1 << a.shift, C::VKEYS);   // keys of a V box
         uint32_t s_phase = 0, turn = 0, uses[2] = {0, 0};   // uses: of the weights' buffers, before this item
-        long long seq = 0;                              // ring slots of the items before this one
+        long long seq = 0;                              // V slots of the items before this one
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
         // any score but does not make NaN of a masked one (-infinity)
         const float scale = a.scale_log2 == 0.f ? 1e-37f : fabsf(a.scale_log2);
@@ -305,7 +310,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             const int live_rows = li.rows_tok * a.G - it.tile * C::ROWS;
             const int nt = C::TILES == 2 && live_rows > 128 ? 2 : 1;
             if (t >= nt) {
-                seq += (long long)count * C::PER_BLOCK;
+                seq += (long long)count * C::VC;
                 continue;
             }
             // ---- queries: 16 bytes per thread and step, rows without a query are zero
@@ -363,11 +368,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     // neighbouring phases apart: the slots' earlier use is known to be over when the product before is.)
                     if (j > 0) wait_product(j - 1);
                     for (int c = 0; c < C::VC; ++c) {
-                        const long long at = seq + C::v_at(j, count) + c;
-                        const uint32_t s = (uint32_t)(at % NS);
+                        const long long at = seq + j * C::VC + c;
+                        const uint32_t s = C::NK + (uint32_t)(at % C::NV);
                         const int from = max(0, li.n - key0 - c * C::VKEYS);
                         if (from >= C::VKEYS) continue;
-                        if (ok) ok = mbar_wait(full(s), (uint32_t)(at / NS) & 1, abort_flag);
+                        if (ok) ok = mbar_wait(full(s), (uint32_t)(at / C::NV) & 1, abort_flag);
                         for (int i = tid; i < (C::VKEYS - from) * PIECES; i += TILE_THREADS) {
                             const int r = from + i / PIECES, piece = i % PIECES;
                             sts128(s_ring + s * C::SLOT + (r / vbox) * vbox * (D * 2) + ((piece / 8) * vbox + r % vbox) * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
@@ -559,7 +564,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             // (the loads above precede this pair's next exchange, and with it the weights that let the next item's
             // product overwrite O)
             tc_fence_before_sync();
-            seq += (long long)count * C::PER_BLOCK;
+            seq += (long long)count * C::VC;
         }
     }
 
