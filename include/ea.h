@@ -531,8 +531,8 @@ int64_t ea_n_floor(int64_t n_kept, double safeguard);
  * touches no memory outside the buffers described here.
  *
  * Limits (EA_ERR_UNSUPPORTED beyond): page_rows 16, 32, 64 or 128; head_dim 64,
- * 128 or 256; n_seqs * n_kv_heads <= 65535; n_pages * page_rows and max_pages *
- * page_rows < 2^31.  The calls that use the context's workspace need
+ * 128 or 256; n_seqs * n_kv_heads <= 65535; n_pages * page_rows < 2^31;
+ * max_pages * page_rows <= 2^30; n_tokens * n_q_heads < 2^31.  The calls that use the context's workspace need
  * ea_paged_workspace_bytes (EA_ERR_WORKSPACE otherwise).  They end the validity
  * of a fused statistics operand (ea_set_fused_stats), which lives there too.
  */
@@ -580,7 +580,8 @@ ea_status ea_paged_workspace_bytes(const ea_paged_shape* shape, int32_t max_q, s
  * beyond max_pages * page_rows, the new rows exceed slot_capacity, or (by token) the
  * heads of a sequence gain different numbers of rows, EA_ERR_PAGES is recorded,
  * the table and the free list stay as they are, every slot is -1 and every
- * offset 0.
+ * offset 0.  (A page number outside the pool in an entry that is given back, or in
+ * the free list, is recorded too, and moves like any other.)
  */
 ea_status ea_page_plan(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old_lens,
                        const int32_t* new_lens, int32_t* block_table, int32_t* free_pages,
@@ -642,7 +643,9 @@ ea_status ea_page_load(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* 
  * scale      finite (1/sqrt(d) as a rule)
  * out        bf16 [n_tokens, Hq, d] dense, 16-byte aligned;  lse_opt fp32 [n_tokens, Hq] or NULL
  * Scores, softmax and sums are fp32; the weights are rounded to bf16 for the
- * product with V, whose accumulation is fp32.  Results do not depend on timing.
+ * product with V, whose accumulation is fp32.  The key blocks of the call are divided
+ * evenly among the SMs, so how the sums of a sequence are grouped depends on all
+ * lengths of the call; the same call gives the same bits.
  */
 ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape, const void* q,
                              int64_t q_stride, int32_t n_tokens, const int32_t* q_offsets,

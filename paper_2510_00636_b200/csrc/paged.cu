@@ -158,6 +158,7 @@ __device__ void move_pages(const PlanArgs& a, const Totals& tot, const int32_t* 
         } else {
             page = a.free_pages[tot.top - 1 - (t - tot.n_give)];
         }
+        if ((unsigned)page >= (unsigned)a.n_pages) a.status[1] = (int)EA_ERR_PAGES;     // the caller's table or free list is wrong
         if (t < tot.n_take) {
             const int r = find_list(take, a.lists, t);
             a.table[(size_t)r * a.max_pages + pages_of(a.old_lens[r], a.shift) + (t - take[r])] = page;
@@ -486,7 +487,7 @@ ea_status ea_check_paged_shape(const ea_paged_shape* s) {
     if (s->page_rows != 16 && s->page_rows != 32 && s->page_rows != 64 && s->page_rows != 128) return EA_ERR_UNSUPPORTED;
     if ((long long)s->n_seqs * s->n_kv_heads > 65535LL) return EA_ERR_UNSUPPORTED;
     // slot numbers and list lengths are 32-bit
-    if ((long long)s->n_pages * s->page_rows > 0x7fffffffLL || (long long)s->max_pages * s->page_rows > 0x7fffffffLL) return EA_ERR_UNSUPPORTED;
+    if ((long long)s->n_pages * s->page_rows > 0x7fffffffLL || (long long)s->max_pages * s->page_rows > (1LL << 30)) return EA_ERR_UNSUPPORTED;
     return EA_OK;
 }
 

@@ -33,7 +33,7 @@ def shape(ea, **changes):
     (dict(n_seqs=-1), INVALID), (dict(n_q_heads=0), INVALID), (dict(n_kv_heads=0), INVALID), (dict(n_kv_heads=3), INVALID),
     (dict(n_pages=-1), INVALID), (dict(max_pages=-1), INVALID), (dict(head_dim=96), UNSUPPORTED), (dict(page_rows=8), UNSUPPORTED),
     (dict(page_rows=48), UNSUPPORTED), (dict(page_rows=0), UNSUPPORTED), (dict(n_seqs=32768), UNSUPPORTED),
-    (dict(n_pages=1 << 27), UNSUPPORTED), (dict(max_pages=1 << 27), UNSUPPORTED),
+    (dict(n_pages=1 << 27), UNSUPPORTED), (dict(max_pages=1 << 27), UNSUPPORTED), (dict(max_pages=(1 << 26) + 1), UNSUPPORTED),
 ])
 def test_shapes_that_do_not_fit_are_refused_by_every_call(ea, ctx, changes, status):
     L, s = ea.lib(), shape(ea, **changes)
