@@ -667,29 +667,31 @@ def ea_paged_workspace_bytes(shape: PagedShape, max_q: int = 1) -> int:
 
 
 def _address(t, dtype, sizes, device, name):
-    """Device address of a contiguous tensor of the given type, sizes and device (None: any sizes)."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() < 0 or not t.is_contiguous():
+    """Device address of a contiguous tensor of the given type, sizes (None: any) and device."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a tensor")
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and (sizes is None or t.shape == sizes):
+        return t.data_ptr()
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
-    if sizes is not None and t.shape != sizes:
-        raise ValueError(f"{name}: expected shape {list(sizes)}, got {list(t.shape)}")
     if t.get_device() != device:
         raise ValueError(f"{name}: a tensor on {t.device} in a call of a context on cuda:{device}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: expected shape {list(sizes)}, got {list(t.shape)}")
 
 
 def _raw_stream(device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _slot_map(shape, order, n_slots, slots, offsets, device):
+def _slot_map(shape, order, n_slots, slots, offsets, device, like):
     """(slots, offsets) as given or new, and their addresses."""
     n = (shape.n_seqs if order == SLOTS_BY_TOKEN else shape.n_seqs * shape.n_kv_heads) + 1
     if slots is None:
-        slots = torch.empty(int(n_slots), dtype=torch.int32, device=f"cuda:{device}")
+        slots = like.new_empty((int(n_slots),))
     elif slots.dim() != 1:
         raise ValueError("slots: expected one dimension")
     if offsets is None:
-        offsets = torch.empty(n, dtype=torch.int32, device=f"cuda:{device}")
+        offsets = like.new_empty((n,))
     return slots, offsets, _address(slots, torch.int32, None, device, "slots"), _address(offsets, torch.int32, (n,), device, "offsets")
 
 
@@ -708,7 +710,7 @@ def ea_page_plan(ctx: Context, shape: PagedShape, old_lens, new_lens, block_tabl
     capacity = 0
     want = n_slots is not None or slots is not None
     if want:
-        slots, offsets, a_slots, a_off = _slot_map(shape, order, n_slots, slots, offsets, dev)
+        slots, offsets, a_slots, a_off = _slot_map(shape, order, n_slots, slots, offsets, dev, old_lens)
         capacity = slots.shape[0]
     elif offsets is not None:
         raise ValueError("offsets: given without n_slots or slots")
@@ -726,7 +728,7 @@ def ea_page_slots(ctx: Context, shape: PagedShape, block_table, first_row, end_r
     a_end = _address(end_row, i32, (S, Hkv), dev, "end_row")
     if n_slots is None and slots is None:
         raise ValueError("ea_page_slots: give n_slots or slots")
-    slots, offsets, a_slots, a_off = _slot_map(shape, order, n_slots, slots, offsets, dev)
+    slots, offsets, a_slots, a_off = _slot_map(shape, order, n_slots, slots, offsets, dev, first_row)
     _check(lib().ea_page_slots(ctx._h, ctypes.byref(shape), a_table, a_first, a_end, order, a_slots, slots.shape[0], a_off,
                                _raw_stream(dev)), "ea_page_slots")
     return slots, offsets
