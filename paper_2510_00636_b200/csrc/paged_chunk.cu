@@ -26,25 +26,28 @@ namespace {
 constexpr float kRescale = 8.0f;
 
 template <int D> struct Chunk {
-    static constexpr int TILES = D == 256 ? 1 : 2;
+    static constexpr bool PAIR = D == 256;              // two CTAs of a cluster work as one
+    static constexpr int TILES = PAIR ? 1 : 2;          // row tiles of a CTA
     static constexpr int HALVES = 2 / TILES;            // threads per row (each has 64 keys of a block)
-    static constexpr int ROWS = TILES * 128;
+    static constexpr int ROWS = 256;
     static constexpr int BK = HALVES * 64;              // keys per block
-    // a slot of its ring: K: all keys of a block x KW * 64 channels;  V: VKEYS keys x all channels
+    // a slot of its ring: K: KROWS keys x KW * 64 channels;  V: VKEYS keys x VCH channels (a CTA of a pair: half the keys of
+    // a block for K, half the channels for V)
     static constexpr uint32_t SLOT = D == 64 ? 8192 : 16384;
-    static constexpr int KW = (int)SLOT / (BK * 128), KC = D / 64 / KW;
-    static constexpr int VKEYS = (int)SLOT / (D * 2), VC = BK / VKEYS;
+    static constexpr int KROWS = PAIR ? BK / 2 : BK, KW = (int)SLOT / (KROWS * 128), KC = D / 64 / KW;
+    static constexpr int VCH = PAIR ? D / 2 : D, VKEYS = (int)SLOT / (VCH * 2), VC = BK / VKEYS;
     static constexpr uint32_t Q_TILE = 128u * D * 2;
     static constexpr int NSLOT = D == 64 ? 20 : D == 128 ? 10 : 9, NV = NSLOT / 2, NK = NSLOT - NV;   // K's ring, then V's
+    static constexpr int PARTS = PAIR ? kPagedMaxCtas : 2 * kPagedMaxCtas;             // places for parts of a row tile
     static constexpr int THREADS = 128 + 256;           // warps 0 and 3 (K, V), 1 and 2 (MMA of a row tile), then the softmax warps
-    static constexpr int BARS = 2 * NSLOT + 16;
-    static constexpr int TAIL_WALK = BARS * 8 + 16;
+    static constexpr int BARS = 2 * NSLOT + 18;
+    static constexpr int TAIL_WALK = (BARS * 8 + 16 + 7) / 8 * 8;
     static constexpr int TAIL_STATS = TAIL_WALK + (int)sizeof(Walk);
     static constexpr int TAIL = TAIL_STATS + (HALVES == 2 ? 2 * 2 * 128 * 4 : 0);      // [turn][half][row]
     static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)SLOT + TAIL;
     static constexpr uint32_t O_COL = 256;              // tensor memory: S of tile t at 2 t BK, P of buffer b BK + b BK / 2 on, O from 256
     static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
-    static_assert(KC * KW * 64 == D && VC * VKEYS == BK && VKEYS % 16 == 0, "slots");
+    static_assert(KC * KW * 64 == D && VC * VKEYS == BK && VKEYS % 16 == 0 && NV >= VC && NK >= KC && (!PAIR || NV < 3 * VC), "slots");
 };
 
 // A place in the ring: slot, and the parity of its use.
@@ -78,11 +81,21 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     auto o_done = [&](int t, int b) { return bars + 8u * (2 * NS + 8 + 2 * t + b); };
     auto q_full = [&](int t) { return bars + 8u * (2 * NS + 12 + t); };
     auto drained = [&](int t) { return bars + 8u * (2 * NS + 14 + t); };      // only used when a wait has given up
+    // (pair) V of the blocks that reach behind their list, on this CTA's own barriers, in turn: V's ring holds two blocks
+    auto v_tail = [&](uint32_t use) { return bars + 8u * (2 * NS + 16 + (use & 1)); };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail + 8 * C::BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8 * C::BARS + 4);
     volatile int* last_flag = abort_flag + 1;           // per row tile: this CTA joins its parts
     Walk* start = reinterpret_cast<Walk*>(tail + C::TAIL_WALK);
 
+    // in a pair: this CTA's place, and what stands for a CTA elsewhere
+    const int rank = C::PAIR ? (int)cluster_ctarank() : 0;
+    const int worker = C::PAIR ? (int)blockIdx.x / 2 : (int)blockIdx.x, workers = C::PAIR ? (int)gridDim.x / 2 : (int)gridDim.x;
+    // an arrival on the MMA issuer's barrier
+    auto tell = [&](uint32_t bar) {
+        if (C::PAIR) mbar_arrive_cluster(mapa(bar, 0));
+        else mbar_arrive(bar);
+    };
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) {
@@ -91,26 +104,33 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         }
         for (int t = 0; t < 2; ++t) {
             for (int b = 0; b < 2; ++b) {
-                mbar_init(p_full(t, b), 4 * C::HALVES);
+                mbar_init(p_full(t, b), C::PAIR ? 16 : 4);
                 mbar_init(o_done(t, b), 1);
             }
             mbar_init(s_full(t), 1);
-            mbar_init(s_read(t), 4 * C::HALVES);
-            mbar_init(q_full(t), 4 * C::HALVES);
+            mbar_init(s_read(t), C::PAIR ? 16 : 4);
+            mbar_init(q_full(t), C::PAIR ? 16 : 4);
             mbar_init(drained(t), 1);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(v_tail(i), C::VC);
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
     }
     if (warp == 1) {
-        tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
-        tmem_relinquish();
+        if (C::PAIR) {
+            tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+            tmem_relinquish_pair();
+        } else {
+            tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+            tmem_relinquish();
+        }
     }
-    find_range<C::THREADS>(a, BK, C::ROWS, blockIdx.x, gridDim.x, start);
+    find_range<C::THREADS>(a, BK, C::ROWS, worker, workers, start);
     tc_fence_before_sync();
     __syncthreads();
+    if (C::PAIR) cluster_sync();                        // the peer's barriers exist before anything signals them
     tc_fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     Walk walk = *start;
@@ -121,11 +141,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     auto feed = [&](auto is_v) {
         constexpr bool V = decltype(is_v)::value;
         // a slot: ROWS keys and WIDE times 64 channels; CHUNKS of them a block
-        constexpr int ROWS = V ? C::VKEYS : BK, WIDE = V ? D / 64 : C::KW, CHUNKS = V ? C::VC : C::KC;
+        constexpr int ROWS = V ? C::VKEYS : C::KROWS, WIDE = V ? C::VCH / 64 : C::KW, CHUNKS = V ? C::VC : C::KC;
         constexpr int FIRST = V ? C::NK : 0, END = V ? NS : C::NK, MAX_SHIFT = ROWS == 128 ? 7 : ROWS == 64 ? 6 : 5;
         const uint32_t leader = elect_one();
         const int box_shift = min(a.shift, MAX_SHIFT), row_mask = (1 << a.shift) - 1;      // keys of a box
         Ring ring = {FIRST, 0};
+        uint32_t tails = 0;
         while (next_item(a, walk, C::ROWS, BK, it)) {
             const int n = it.li.n;
             const int entries = (int)(((unsigned)n + (1u << a.shift) - 1u) >> a.shift);
@@ -152,27 +173,44 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 }
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
-                    const int key0 = b * BK + (V ? c * ROWS : 0), rest = n - key0;
-                    const int boxes = rest <= 0 ? 0 : min(ROWS >> box_shift, (rest + (1 << box_shift) - 1) >> box_shift);
+                    const int key0 = b * BK + (V ? c * ROWS : rank * ROWS), rest = n - key0;
+                    auto boxes_of = [&](int left) { return left <= 0 ? 0 : min(ROWS >> box_shift, (left + (1 << box_shift) - 1) >> box_shift); };
+                    const int boxes = boxes_of(rest);
                     if (ok) ok = mbar_wait(empty(ring.slot), ring.phase ^ 1, abort_flag);
                     __syncwarp();
                     const uint32_t go = ok ? leader : 0u;
-                    const uint32_t bar = full(ring.slot), to = s_ring + ring.slot * C::SLOT;
-                    if (go) mbar_arrive_expect_tx(bar, (uint32_t)((boxes * 128 * WIDE) << box_shift));
+                    const uint32_t to = s_ring + ring.slot * C::SLOT;
+                    uint32_t bar = full(ring.slot);
+                    // V rows behind the list's end are made zero by the softmax warps, which in a pair can only wait for this
+                    // CTA's part of the block: it gets a barrier of its own, and the weights' arrival tells the MMA issuer
+                    const bool own = C::PAIR && V && (b + 1) * BK > n;
+                    if (!C::PAIR) {
+                        if (go) mbar_arrive_expect_tx(bar, (uint32_t)((boxes * 128 * WIDE) << box_shift));
+                    } else {
+                        // in a pair the leader's barrier counts both CTAs' bytes: V alike, K the two halves of the keys
+                        const int both = own ? 0 : V ? 2 * boxes : boxes + boxes_of(rest - ROWS);
+                        if (go && rank == 0) mbar_arrive_expect_tx(bar, (uint32_t)((both * 128 * WIDE) << box_shift));
+                        if (go && own) mbar_arrive_expect_tx(v_tail(tails), (uint32_t)((boxes * 128 * WIDE) << box_shift));
+                        bar = own ? v_tail(tails) : mapa(bar, 0);
+                    }
+                    auto load = [&](uint32_t dst, const CUtensorMap* map, int y, int z) {
+                        if (C::PAIR && !own) tma_load_3d_pair_warp(go, dst, map, bar, 0, y, z);
+                        else tma_load_3d_warp(go, dst, map, bar, 0, y, z);
+                    };
 #pragma unroll 2
                     for (int x = 0; x < boxes; ++x) {
                         const int key = key0 + (x << box_shift);
                         const int y = (__shfl_sync(0xffffffffu, cur, ((key >> a.shift) - win) & 31) << a.shift) + (key & row_mask);
                         if (V) {                        // box after box: [64 channels][row][128 bytes] each
-                            tma_load_3d_warp(go, to + ((uint32_t)(x * D * 2) << box_shift), &v_map, bar, 0, y, 0);
+                            load(to + ((uint32_t)(x * C::VCH * 2) << box_shift), &v_map, y, rank * WIDE);
                         } else {                        // the rows of a chunk of 64 channels side by side
 #pragma unroll
-                            for (int w = 0; w < WIDE; ++w)
-                                tma_load_3d_warp(go, to + w * BK * 128 + ((uint32_t)(x * 128) << box_shift), &k_map, bar, 0, y, c * WIDE + w);
+                            for (int w = 0; w < WIDE; ++w) load(to + w * ROWS * 128 + ((uint32_t)(x * 128) << box_shift), &k_map, y, c * WIDE + w);
                         }
                     }
                     ring.next(FIRST, END);
                 }
+                if ((b + 1) * BK > n) ++tails;
             }
         }
         ok = __all_sync(0xffffffffu, ok);
@@ -181,18 +219,25 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 mbar_drain(full(s), 0);
                 mbar_drain(full(s), 1);
             }
+        if (C::PAIR && V && !ok && lane == 0)
+            for (int i = 0; i < 4; ++i) mbar_drain(v_tail(i), i / 2);
         __syncwarp();
     };
     if (warp == 0) {
         feed(std::false_type());
     } else if (warp == 3) {
         feed(std::true_type());
-    } else if (warp <= C::TILES) {
+    } else if (warp <= C::TILES && rank == 0) {
         // ------------------------------------------------------------------------------ MMA issuer of a row tile
         // The whole warp runs this loop in step, and one lane issues (see umma_bf16_warp).
         const int t = warp - 1;
         const uint32_t leader = elect_one();
-        const uint32_t idesc_s = umma_idesc_bf16_m128(BK), idesc_o = umma_idesc_bf16_m128(D) | kIdescBMnMajor;
+        const uint32_t idesc_s = C::PAIR ? umma_idesc_bf16_m256(BK) : umma_idesc_bf16_m128(BK);
+        const uint32_t idesc_o = (C::PAIR ? umma_idesc_bf16_m256(D) : umma_idesc_bf16_m128(D)) | kIdescBMnMajor;
+        auto commit = [&](uint32_t bar) {               // (in a pair: on both CTAs' barriers)
+            if (C::PAIR) umma_commit_pair_warp(leader, bar, 3);
+            else umma_commit_warp(leader, bar);
+        };
         const uint64_t q_desc = umma_desc_k_sw128(s_q + t * C::Q_TILE), k_desc = umma_desc_k_sw128(s_ring);
         // V: a box of `vbox` keys after the other, in it a chunk of 64 channels after the other
         const int vbox = min(1 << a.shift, C::VKEYS), vbits = vbox == C::VKEYS ? 31 : a.shift;
@@ -200,7 +245,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         uint64_t v_step[C::VKEYS / 16];                 // to keys 16 ks ..: box (16 ks) / vbox, row (16 ks) % vbox of it
 #pragma unroll
         for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-            v_step[ks] = (uint32_t)__shfl_sync(0xffffffffu, ((ks * 16 >> vbits) * vbox * (D * 2 - 128) + ks * 2048) >> 4, 0);
+            v_step[ks] = (uint32_t)__shfl_sync(0xffffffffu, ((ks * 16 >> vbits) * vbox * (C::VCH * 2 - 128) + ks * 2048) >> 4, 0);
         const uint32_t s_tmem = tmem + 2 * t * BK, o_tmem = tmem + C::O_COL + t * D;
         uint32_t p_phase = 0, q_phase = 0, r_phase = 0; // parity of the next phase of p_full(t, b) (bit b), q_full, s_read
         Ring k_ring = {0, 0}, v_ring = {(uint32_t)C::NK, 0};
@@ -211,12 +256,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll 1
                 for (int i = 0; i < count; ++i) {
                     for (int c = 0; c < C::KC; ++c) {
-                        if (ok) ok = mbar_wait(full(k_ring.slot), k_ring.phase, abort_flag);
+                        if (ok) ok = mbar_wait<C::PAIR>(full(k_ring.slot), k_ring.phase, abort_flag);
                         if (leader) mbar_arrive(empty(k_ring.slot));
                         k_ring.next(0, C::NK);
                     }
                     for (int c = 0; c < C::VC; ++c) {
-                        if (ok) ok = mbar_wait(full(v_ring.slot), v_ring.phase, abort_flag);
+                        if (ok) ok = mbar_wait<C::PAIR>(full(v_ring.slot), v_ring.phase, abort_flag);
                         if (leader) mbar_arrive(empty(v_ring.slot));
                         v_ring.next(C::NK, NS);
                     }
@@ -224,39 +269,41 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 ok = __all_sync(0xffffffffu, ok);
                 continue;
             }
-            if (ok) ok = mbar_wait(q_full(t), q_phase, abort_flag);
+            if (ok) ok = mbar_wait<C::PAIR>(q_full(t), q_phase, abort_flag);
             q_phase ^= 1;
 #pragma unroll 1
             for (int j = -1; j < count; ++j) {
                 if (j + 1 < count) {                    // S = Q K(j + 1)^T, once the softmax has read the scores before
                     if (j >= 0) {
-                        if (ok) ok = mbar_wait(s_read(t), r_phase, abort_flag);
+                        if (ok) ok = mbar_wait<C::PAIR>(s_read(t), r_phase, abort_flag);
                         r_phase ^= 1;
                     }
 #pragma unroll
                     for (int c = 0; c < C::KC; ++c) {
-                        if (ok) ok = mbar_wait(full(k_ring.slot), k_ring.phase, abort_flag);
+                        if (ok) ok = mbar_wait<C::PAIR>(full(k_ring.slot), k_ring.phase, abort_flag);
                         ok = __all_sync(0xffffffffu, ok);
                         if (ok) {
                             tc_fence_after_sync();
                             const uint64_t qd = q_desc + c * C::KW * (16384 >> 4), kd = k_desc + k_ring.slot * (C::SLOT >> 4);
 #pragma unroll
-                            for (int ks = 0; ks < 4 * C::KW; ++ks)
-                                umma_bf16_warp(leader, s_tmem, qd + (ks / 4) * (16384 >> 4) + ks % 4 * 2, kd + (ks / 4) * (BK * 128 >> 4) + ks % 4 * 2,
-                                               idesc_s, c + ks > 0 ? 1u : 0u);
-                            umma_commit_warp(leader, empty(k_ring.slot));
+                            for (int ks = 0; ks < 4 * C::KW; ++ks) {
+                                const uint64_t q_at = qd + (ks / 4) * (16384 >> 4) + ks % 4 * 2, k_at = kd + (ks / 4) * (C::KROWS * 128 >> 4) + ks % 4 * 2;
+                                if (C::PAIR) umma_bf16_pair_warp(leader, s_tmem, q_at, k_at, idesc_s, c + ks > 0 ? 1u : 0u);
+                                else umma_bf16_warp(leader, s_tmem, q_at, k_at, idesc_s, c + ks > 0 ? 1u : 0u);
+                            }
+                            commit(empty(k_ring.slot));
                         }
                         k_ring.next(0, C::NK);
                     }
-                    if (ok) umma_commit_warp(leader, s_full(t));
+                    if (ok) commit(s_full(t));
                 }
                 if (j >= 0) {                           // O += P(j) V(j)
                     const int b = j & 1;
-                    if (ok) ok = mbar_wait(p_full(t, b), (p_phase >> b) & 1, abort_flag);
+                    if (ok) ok = mbar_wait<C::PAIR>(p_full(t, b), (p_phase >> b) & 1, abort_flag);
                     p_phase ^= 1u << b;
 #pragma unroll
                     for (int c = 0; c < C::VC; ++c) {
-                        if (ok) ok = mbar_wait(full(v_ring.slot), v_ring.phase, abort_flag);
+                        if (ok) ok = mbar_wait<C::PAIR>(full(v_ring.slot), v_ring.phase, abort_flag);
                         ok = __all_sync(0xffffffffu, ok);
                         if (ok) {
                             tc_fence_after_sync();
@@ -264,17 +311,18 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                             const uint32_t p_tmem = s_tmem + BK + b * (BK / 2) + c * (C::VKEYS / 2);
 #pragma unroll
                             for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-                                umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
-                            umma_commit_warp(leader, empty(v_ring.slot));
+                                if (C::PAIR) umma_bf16_ts_pair_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
+                                else umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
+                            commit(empty(v_ring.slot));
                         }
                         v_ring.next(C::NK, NS);
                     }
-                    if (ok) umma_commit_warp(leader, o_done(t, b));
+                    if (ok) commit(o_done(t, b));
                 }
             }
         }
         if (!ok) {                                      // MMAs in flight end before the tensor memory goes back
-            umma_commit_warp(leader, drained(t));
+            commit(drained(t));
             mbar_drain(drained(t), 0);
         }
         __syncwarp();
@@ -291,7 +339,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * OWN;
         float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS);
         const int vbox = min(1 << a.shift, C::VKEYS);   // keys of a V box
-        uint32_t s_phase = 0, turn = 0, uses[2] = {0, 0};   // uses: of the weights' buffers, before this item
+        const int part_tile = C::PAIR ? rank : t;       // which 128 of a row tile's rows
+        uint32_t s_phase = 0, turn = 0, tails = 0, uses[2] = {0, 0};   // uses: of the weights' buffers, before this item
         long long seq = 0;                              // V slots of the items before this one
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
         // any score but does not make NaN of a masked one (-infinity)
@@ -315,7 +364,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
             // ---- queries: 16 bytes per thread and step, rows without a query are zero
             const int head0 = (it.list - quotient(it.list, a.div_hkv) * a.Hkv) * a.G;
-            const int row0 = it.tile * C::ROWS + t * 128;
+            const int row0 = it.tile * C::ROWS + part_tile * 128;
             constexpr int PIECES = D / 8, STEPS = 128 * PIECES / TILE_THREADS, BATCH = STEPS < 8 ? STEPS : 8;
             // (the same thread that stored an output piece in this place, so the place is free)
             const uint32_t q_tile = s_q + t * C::Q_TILE;
@@ -345,13 +394,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(q_full(t));
+            if (lane == 0) tell(q_full(t));
 
             const int tok = quotient(row0 + row, a.div_g);
             const bool live = tok < li.rows_tok;
             const int lim = live ? limit_of(li, a, tok) : 0;
             // keys that every row of the tile sees
-            const int seen = limit_of(li, a, quotient(row0, a.div_g));
+            const int seen = limit_of(li, a, min(quotient(row0, a.div_g), li.rows_tok - 1));
             float m = -INFINITY, l = 0.f;
             // the product of block j has ended
             auto wait_product = [&](int j) {
@@ -366,16 +415,22 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN: they become
                     // zero before the weights let the product go (by both tiles: the zeros are the same).  (A parity tells two
                     // neighbouring phases apart: the slots' earlier use is known to be over when the product before is.)
-                    if (j > 0) wait_product(j - 1);
+                    if (C::PAIR) {
+                        if (ok) ok = mbar_wait(v_tail(tails), (tails >> 1) & 1, abort_flag);
+                        ++tails;
+                    } else if (j > 0) {
+                        wait_product(j - 1);
+                    }
                     for (int c = 0; c < C::VC; ++c) {
                         const long long at = seq + j * C::VC + c;
                         const uint32_t s = C::NK + (uint32_t)(at % C::NV);
                         const int from = max(0, li.n - key0 - c * C::VKEYS);
                         if (from >= C::VKEYS) continue;
-                        if (ok) ok = mbar_wait(full(s), (uint32_t)(at / C::NV) & 1, abort_flag);
-                        for (int i = tid; i < (C::VKEYS - from) * PIECES; i += TILE_THREADS) {
-                            const int r = from + i / PIECES, piece = i % PIECES;
-                            sts128(s_ring + s * C::SLOT + (r / vbox) * vbox * (D * 2) + ((piece / 8) * vbox + r % vbox) * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
+                        if (!C::PAIR && ok) ok = mbar_wait(full(s), (uint32_t)(at / C::NV) & 1, abort_flag);
+                        constexpr int V_PIECES = C::VCH / 8;
+                        for (int i = tid; i < (C::VKEYS - from) * V_PIECES; i += TILE_THREADS) {
+                            const int r = from + i / V_PIECES, piece = i % V_PIECES;
+                            sts128(s_ring + s * C::SLOT + (r / vbox) * vbox * (C::VCH * 2) + ((piece / 8) * vbox + r % vbox) * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
                         }
                     }
                     fence_proxy_async_smem();
@@ -388,7 +443,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 tmem_ld_x32(s_col + half * 64 + 32, x[1]);
                 tmem_ld_wait();                         // (of the whole warp)
                 tc_fence_before_sync();
-                if (lane == 0 && j + 1 < count) mbar_arrive(s_read(t));
+                if (lane == 0 && j + 1 < count) tell(s_read(t));
                 if (key0 + BK > seen) {
                     const int local = lim - key0 - half * 64;
 #pragma unroll
@@ -450,7 +505,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 if (nt == 2 && (t == 0 || j + 1 < count)) bar_arrive(7 + (t ^ 1) * 4 + quarter, 64);
                 tmem_st_wait();
                 tc_fence_before_sync();
-                if (lane == 0) mbar_arrive(p_full(t, b));
+                if (lane == 0) tell(p_full(t, b));
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
             // ---- output: with two threads per row each its channels
@@ -482,12 +537,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 }
             } else {
                 // a part: [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) write side by side
-                const Shared sh = shared_by(it, walk.total, gridDim.x);
-                const int own = 2 * (int)blockIdx.x + (it.first ? 0 : 1);
-                float* part = a.part_o + (half * OWN * C::ROWS + (t * 128 + row) * 4);
-                float2* ml = reinterpret_cast<float2*>(a.part_ml) + t * 128 + row;
+                const Shared sh = shared_by(it, walk.total, workers);
+                const int own = 2 * worker + (it.first ? 0 : 1);
+                float* part = a.part_o + (half * OWN * C::ROWS + (part_tile * 128 + row) * 4);
+                float2* ml = reinterpret_cast<float2*>(a.part_ml) + part_tile * 128 + row;
                 // if all others have arrived, this part need not be written
-                if (tid == 0) last_flag[t] = others_arrived(a.counters + 2 * sh.c0 + t, sh.parts) ? 1 : 0;
+                if (tid == 0) last_flag[t] = others_arrived(a.counters + 2 * sh.c0 + part_tile, sh.parts) ? 1 : 0;
                 bar_sync(5 + t, TILE_THREADS);
                 write = last_flag[t] != 0;
                 if (!write) {
@@ -502,7 +557,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     }
                     if (half == 0) ml[(size_t)own * C::ROWS] = make_float2(m, l);
                     bar_sync(5 + t, TILE_THREADS);
-                    if (tid == 0) last_flag[t] = arrives_last(a.counters + 2 * sh.c0 + t, sh.parts) ? 1 : 0;
+                    if (tid == 0) last_flag[t] = arrives_last(a.counters + 2 * sh.c0 + part_tile, sh.parts) ? 1 : 0;
                     bar_sync(5 + t, TILE_THREADS);
                     write = last_flag[t] != 0;
                 }
@@ -570,9 +625,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 
     tc_fence_before_sync();
     __syncthreads();
+    if (C::PAIR) cluster_sync();                        // the peer's MMAs and signals reach into this CTA until here
     if (warp == 1) {
         tc_fence_after_sync();
-        tmem_dealloc(tmem, 512);
+        if (C::PAIR) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 512);
     }
     if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
 }
@@ -581,24 +638,39 @@ template <int D>
 ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& args, const void* k_pages, const void* v_pages, cudaStream_t st) {
     using C = Chunk<D>;
     AttnArgs a = args;
-    const int ctas = ctx->sm_count < kPagedMaxCtas ? ctx->sm_count : kPagedMaxCtas;
+    const int sms = ctx->sm_count < kPagedMaxCtas ? ctx->sm_count : kPagedMaxCtas, ctas = C::PAIR ? sms / 2 * 2 : sms;
     a.part_o = static_cast<float*>(ctx->workspace);
-    a.part_ml = a.part_o + (size_t)2 * kPagedMaxCtas * C::ROWS * D;
+    a.part_ml = a.part_o + (size_t)C::PARTS * C::ROWS * D;
     CUtensorMap k_map, v_map;
-    const uint32_t kbox = s.page_rows < C::BK ? (uint32_t)s.page_rows : (uint32_t)C::BK, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
-    if (!ea_paged_map(ctx, s, k_pages, kbox, 1, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, D / 64, &v_map)) return EA_ERR_CUDA;
+    const uint32_t kbox = s.page_rows < C::KROWS ? (uint32_t)s.page_rows : (uint32_t)C::KROWS, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
+    if (!ea_paged_map(ctx, s, k_pages, kbox, 1, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, C::VCH / 64, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_chunk_kernel<D>;
     static std::atomic<uint64_t> done{0};
     ea_status err = ea_allow_smem(kernel, C::SMEM, ctx->device, done);
     if (err != EA_OK) return err;
-    kernel<<<ctas, C::THREADS, C::SMEM, st>>>(k_map, v_map, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C::PAIR ? 2 : 1;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    EA_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, k_map, v_map, a));
     ea_count_launches(ctx, 1);
     return EA_CHECK_LAUNCH();
 }
 
 }  // namespace
 
-size_t ea_paged_chunk_ws_floats(int d) { return (size_t)2 * kPagedMaxCtas * (d == 256 ? 128 : 256) * (d + 2); }
+size_t ea_paged_chunk_ws_floats(int d) {
+    const int parts = d == 64 ? Chunk<64>::PARTS : d == 128 ? Chunk<128>::PARTS : Chunk<256>::PARTS;
+    return (size_t)parts * Chunk<64>::ROWS * (d + 2);
+}
 
 ea_status ea_launch_paged_chunk(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& a, const void* k_pages, const void* v_pages,
                                 cudaStream_t st) {
