@@ -523,7 +523,76 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                                       pack_bf16(o[e + 4] * f, o[e + 5] * f), pack_bf16(o[e + 6] * f, o[e + 7] * f)));
             };
             bool write = true;
-            if (it.b0 == 0 && it.b1 == it.blocks) {
+            if (it.b0 != 0 || it.b1 != it.blocks) {
+                // A part.  Neighbours join in pairs, pairs of pairs and so on, the second to arrive at a pair taking the first
+                // one's sum in: log2(parts) steps, each on all SMs that the tile's parts are on, and in an order that does not
+                // depend on who arrives when.  [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) lie side by side.
+                const Shared sh = shared_by(it, walk.total, workers);
+                float* part = a.part_o + (half * OWN * C::ROWS + (part_tile * 128 + row) * 4);
+                float2* ml = reinterpret_cast<float2*>(a.part_ml) + part_tile * 128 + row;
+                const bool busy = part_tile * 128 + quarter * 32 < live_rows;      // the warp has a row that is one
+                int lo = worker - sh.c0;                // this sum: parts lo .. lo + span - 1 (those that there are)
+                for (int span = 1; span < sh.parts && write; span *= 2) {
+                    const bool right = lo & span;
+                    const int other = right ? lo - span : lo + span;
+                    if (other >= sh.parts) continue;
+                    // (a CTA is the first part of a right side in one tile at most, so its counters name the pair)
+                    unsigned* counter = a.counters + 2 * (sh.c0 + (right ? lo : other)) + part_tile;
+                    // if the other has arrived, this sum need not be written
+                    if (tid == 0) last_flag[t] = others_arrived(counter, 2) ? 1 : 0;
+                    bar_sync(5 + t, TILE_THREADS);
+                    write = last_flag[t] != 0;
+                    if (!write) {
+                        const size_t to = (size_t)sh.slot(lo) * C::ROWS;
+#pragma unroll 1
+                        for (int c = 0; busy && c < OWN; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld_x32(o_col + c, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<uint4*>(part + to * D + (c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        }
+                        if (half == 0) ml[to] = make_float2(m, l);
+                        bar_sync(5 + t, TILE_THREADS);
+                        if (tid == 0) last_flag[t] = arrives_last(counter, 2) ? 1 : 0;
+                        bar_sync(5 + t, TILE_THREADS);
+                        write = last_flag[t] != 0;
+                    }
+                    if (write) {
+                        const size_t from = (size_t)sh.slot(other) * C::ROWS;
+                        const float2 y = __ldcg(ml + from);
+                        const float m_new = fmaxf(m, y.x), z = m_new == -INFINITY ? 0.f : m_new;
+                        const float f = ex2(m - z), fy = ex2(y.x - z);
+                        m = m_new;
+                        // (no fused multiply: either side may be the one that adds)
+                        auto joined = [&](float mine, float theirs) { return __fadd_rn(__fmul_rn(mine, f), __fmul_rn(theirs, fy)); };
+                        l = joined(l, y.y);
+#pragma unroll 1
+                        for (int c = 0; busy && c < OWN; c += 32) {
+                            float4 v[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = __ldcg(reinterpret_cast<const float4*>(part + from * D + (c + 4 * e) * C::ROWS));
+                            uint32_t o[32];
+                            tmem_ld_x32(o_col + c, o);
+                            tmem_ld_wait();
+                            auto add = [&](uint32_t& at, float x) { at = __float_as_uint(joined(__uint_as_float(at), x)); };
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                add(o[4 * e], v[e].x);
+                                add(o[4 * e + 1], v[e].y);
+                                add(o[4 * e + 2], v[e].z);
+                                add(o[4 * e + 3], v[e].w);
+                            }
+                            tmem_st_x32(o_col + c, o);
+                        }
+                        tmem_st_wait();
+                        bar_sync(5 + t, TILE_THREADS);  // (last_flag is written again)
+                    }
+                    lo = min(lo, other);
+                }
+            }
+            if (write) {
                 const float inv = inverse_sum(l);
 #pragma unroll 1
                 for (int c = 0; c < OWN; c += 32) {
@@ -534,74 +603,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll
                     for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(o[e]);
                     stage(c, f, inv);
-                }
-            } else {
-                // a part: [D / 4][ROWS][4 channels], so that the lanes of a warp (rows) write side by side
-                const Shared sh = shared_by(it, walk.total, workers);
-                const int own = 2 * worker + (it.first ? 0 : 1);
-                float* part = a.part_o + (half * OWN * C::ROWS + (part_tile * 128 + row) * 4);
-                float2* ml = reinterpret_cast<float2*>(a.part_ml) + part_tile * 128 + row;
-                // if all others have arrived, this part need not be written
-                if (tid == 0) last_flag[t] = others_arrived(a.counters + 2 * sh.c0 + part_tile, sh.parts) ? 1 : 0;
-                bar_sync(5 + t, TILE_THREADS);
-                write = last_flag[t] != 0;
-                if (!write) {
-#pragma unroll 1
-                    for (int c = 0; c < OWN; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld_x32(o_col + c, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4*>(part + (size_t)own * C::ROWS * D + (c + e) * C::ROWS) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                    }
-                    if (half == 0) ml[(size_t)own * C::ROWS] = make_float2(m, l);
-                    bar_sync(5 + t, TILE_THREADS);
-                    if (tid == 0) last_flag[t] = arrives_last(a.counters + 2 * sh.c0 + part_tile, sh.parts) ? 1 : 0;
-                    bar_sync(5 + t, TILE_THREADS);
-                    write = last_flag[t] != 0;
-                }
-                if (write) {
-                    const float m_own = m, l_own = l;
-                    auto stats_of = [&](int p) { return sh.slot(p) == own ? make_float2(m_own, l_own) : __ldcg(ml + (size_t)sh.slot(p) * C::ROWS); };
-                    for (int p = 0; p < sh.parts; ++p) m = fmaxf(m, stats_of(p).x);
-                    const float z = m == -INFINITY ? 0.f : m;
-                    l = 0.f;
-                    for (int p = 0; p < sh.parts; ++p) {
-                        const float2 v = stats_of(p);
-                        l += v.y * ex2(v.x - z);
-                    }
-                    const float inv = inverse_sum(l);
-#pragma unroll 1
-                    for (int c = 0; c < OWN; c += 32) {
-                        float o[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0.f;
-#pragma unroll 1
-                        for (int p = 0; p < sh.parts; ++p) {       // in the order of the keys, this CTA's own from where it is
-                            const float w = ex2(stats_of(p).x - z);
-                            if (sh.slot(p) == own) {
-                                uint32_t v[32];
-                                tmem_ld_x32(o_col + c, v);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] += __uint_as_float(v[e]) * w;
-                            } else {
-                                const float* src = part + (size_t)sh.slot(p) * C::ROWS * D + c * C::ROWS;
-                                float4 v[8];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] = __ldcg(reinterpret_cast<const float4*>(src + e * 4 * C::ROWS));
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    o[4 * e] += v[e].x * w;
-                                    o[4 * e + 1] += v[e].y * w;
-                                    o[4 * e + 2] += v[e].z * w;
-                                    o[4 * e + 3] += v[e].w * w;
-                                }
-                            }
-                        }
-                        stage(c, o, inv);
-                    }
                 }
             }
             if (write) {
