@@ -532,9 +532,10 @@ int64_t ea_n_floor(int64_t n_kept, double safeguard);
  *
  * Limits (EA_ERR_UNSUPPORTED beyond): page_rows 16, 32, 64 or 128; head_dim 64,
  * 128 or 256; n_seqs * n_kv_heads <= 65535; n_pages * page_rows < 2^31;
- * max_pages * page_rows <= 2^30; n_tokens * n_q_heads < 2^31.  The calls that use the context's workspace need
- * ea_paged_workspace_bytes (EA_ERR_WORKSPACE otherwise).  They end the validity
- * of a fused statistics operand (ea_set_fused_stats), which lives there too.
+ * max_pages * page_rows <= 2^30; n_tokens * n_q_heads < 2^31.  The calls that use
+ * the context's workspace need ea_paged_workspace_bytes (EA_ERR_WORKSPACE
+ * otherwise).  They end the validity of a fused statistics operand
+ * (ea_set_fused_stats), which lives there too.
  */
 typedef struct ea_paged_shape {
     int32_t n_seqs;      /* sequences in this call (or (layer, sequence) units)        */

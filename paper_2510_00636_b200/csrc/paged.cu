@@ -16,10 +16,18 @@
 
 namespace {
 
+// Four paths, times on the device for a plan that grows lists and one that takes the pages back, in a CUDA graph:
+//  * a plan with a slot map of at most kClusterSlots slots: one cluster, one launch.  8 lists x 64 rows 10.0 us, 65 536 slots
+//    13.3 (13.6 with three launches); beyond, the slots want all SMs: 131 072 slots 15.1 us against 13.5, 288 000 27.9
+//    against 19.0.  (A single CTA, without cluster barriers, is no faster for small plans: 10.2 us at 512 slots, 12.7
+//    against 10.5 at 8192.)
+//  * a plan without a slot map: one launch over all SMs, as nothing bounds the pages that move but the pool (288 lists
+//    taking 64 800 pages: 30 us for both calls against 38 in a cluster)
+//  * a slot map of standing tables: one launch over all SMs (8.4 us for 288 x 1000 slots with the launch)
+//  * more lists than a CTA keeps prefixes of: scan, pages and slots in three launches
 constexpr int kSelfScanLists = 4096;      // up to here every CTA scans the lengths itself (48 KiB of prefixes)
 constexpr int kScanSmem = 3 * (kSelfScanLists + 1) * 4;
-constexpr int kOneCtaSlots = 8192;        // up to here a plan is one CTA's work
-constexpr int kClusterSlots = 65536;      // up to here it is one cluster's (one launch); beyond, three launches over all SMs
+constexpr int kClusterSlots = 65536, kPlanCluster = 8;
 constexpr int kScanThreads = 1024, kMoveThreads = 256;
 
 struct PlanArgs {
@@ -369,15 +377,14 @@ ea_status launch_plan(const ea_ctx* ctx, PlanArgs a, cudaStream_t st) {
         static std::atomic<uint64_t> done{0};
         const ea_status err = ea_allow_smem(page_plan_cluster_kernel, kScanSmem, ctx->device, done);
         if (err != EA_OK) return err;
-        const unsigned ctas = a.slot_capacity <= kOneCtaSlots ? 1 : 8;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(ctas);
+        cfg.gridDim = dim3(kPlanCluster);
         cfg.blockDim = dim3(kScanThreads);
         cfg.dynamicSmemBytes = (size_t)smem;
         cfg.stream = st;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = ctas;
+        attr[0].val.clusterDim.x = kPlanCluster;
         attr[0].val.clusterDim.y = 1;
         attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;

@@ -450,6 +450,34 @@ def test_many_sequences_of_few_rows(ea):
     check(ea, make(ea, (28, 4, 128), 16, [s % 3 for s in range(S)], lens))
 
 
+@pytest.mark.parametrize("heads", [(4, 2, 64), (12, 3, 128), (4, 2, 256), (30, 2, 256)])
+@pytest.mark.parametrize("page", [16, 128])
+def test_many_short_lists_of_chunks(ea, heads, page):
+    S, Hkv = 90, heads[1]
+    chunks = [(5 * s) % 23 for s in range(S)]
+    chunks[7] = 40
+    lens = [[(31 * s + 77 * g) % 140 for g in range(Hkv)] for s in range(S)]
+    check(ea, make(ea, heads, page, chunks, lens))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("m", [17, 127, 128, 129, 255, 256, 257, 511, 513])
+def test_rows_around_the_tiles(ea, d, m):
+    for n in (m, 900):
+        check(ea, make(ea, (2, 2, d), 64, [m, 3], [[n, m + 130], [5, 600]]))
+
+
+@pytest.mark.parametrize("heads", [(5, 1, 64), (5, 1, 128), (5, 1, 256)])
+@pytest.mark.parametrize("n", [700, 5000, 60000])
+def test_few_lists_joined_from_many_parts(ea, heads, n):
+    for m in (4, 30, 100):
+        c = make(ea, heads, 64, [m], [[n]])
+        out, lse = check(ea, c)
+        for _ in range(5):                                   # in whatever order the parts arrive
+            again = attend(ea, c, causal=True, want_lse=True)
+            assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
 # ---- as they are used ------------------------------------------------------------------------------------------------
 def test_on_another_stream_and_with_a_workspace_that_is_too_small(ea):
     c = make(ea, (8, 2, 128), 16, [1, 1], [[200, 300], [40, 50]])
