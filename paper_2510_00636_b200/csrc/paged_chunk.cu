@@ -1,18 +1,30 @@
 // Attention of chunks of new tokens over the paged cache on the tensor cores (tcgen05).
 //
-// A CTA works on row tiles of 128 packed rows (row = token * G + head), two of them at head_dim <= 128, one at 256 (the
-// output of a tile takes head_dim of the 512 tensor-memory columns), against blocks of 64 (two tiles) or 128 keys:
+// A CTA works on row tiles of 128 packed rows (row = token * G + head) against blocks of keys:
 //     S = Q K^T        tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
 //     P = 2^(c S - m)  running maximum m and sum l per row; P (bf16) in tensor memory, two buffers per tile
 //     O += P V         A = P from tensor memory, B = V as it lies (rows are the contraction index: MN-major)
+// head_dim <= 128: two row tiles against blocks of 64 keys (S, P and O of both fill the 512 columns of tensor memory).
+// head_dim 256: O of one tile takes half of them, so there is one tile, against blocks of 128 keys, and two CTAs of a
+// cluster work as one (cta_group::2): 256 rows, each CTA with its 128, half of a block's keys of K and half of V's
+// channels.  What an SM can draw from L2 (26 to 29 bytes per cycle) is the limit there: a CTA alone fetches 64 KiB of K and
+// V for 128 rows and 64 keys, a CTA of the pair half of that (512 tokens over 16 384 keys, 8 lists: 206 -> 122 us).
+//
 // Two warps keep K and V flowing through a ring of slots each (TMA boxes of a page), one warp per row tile issues its MMAs
-// (the waits of one are hidden by the other's), eight warps do the softmax, 64 scores per thread and block.  The scores of
-// the next block are on their way as soon as those of this one have been read.
+// (the waits of one are hidden by the other's; in a pair one warp of the first CTA issues for both), eight warps do the
+// softmax, 64 scores per thread and block.  The scores of the next block are on their way as soon as those of this one
+// have been read.
 //
 // The running maximum only moves when a row's scores exceed it by more than 2^8 (the weights then stay within fp32 and
 // bf16 range, and the sum, which uses the same maximum, cancels it): O is rescaled in tensor memory only then.
 //
 // The CTAs divide the call's (row tile, key block) units evenly, as in the kernel for few rows (paged_attn.cuh).
+//
+// What bounds it at head_dim 128: for 64 keys and two tiles the MMAs take 1280 cycles (Q K^T with N = 64 reads its 128
+// query rows from shared memory for only 64 columns: 48 cycles an instruction where the arithmetic takes 32), the
+// exponentials 1024 of the special function units; the two tiles alternate on both and about 1600 pass.  2048 tokens
+// over 32 768 keys, 32 heads on 8 lists: 880 us = 1.21 PFLOP/s (0.72 of the measured cuBLAS rate); back to back, at the
+// clock that the power limit leaves, 1075 us (0.71 of the rate measured there).
 #include <type_traits>
 
 #include "paged.h"
@@ -23,7 +35,7 @@ using namespace ptx;
 
 namespace {
 
-constexpr float kRescale = 8.0f;
+constexpr float kRescale = 8.0f;          // log2 of how far a row's scores may exceed its running maximum
 
 template <int D> struct Chunk {
     static constexpr bool PAIR = D == 256;              // two CTAs of a cluster work as one
