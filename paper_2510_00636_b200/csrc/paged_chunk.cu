@@ -13,7 +13,9 @@
 // Two warps keep K and V flowing through a ring of slots each (TMA boxes of a page), one warp per row tile issues its MMAs
 // (the waits of one are hidden by the other's; in a pair one warp of the first CTA issues for both), eight warps do the
 // softmax, 64 scores per thread and block.  The scores of the next block are on their way as soon as those of this one
-// have been read.
+// have been read.  A row tile of at most 128 rows leaves the second place of a CTA free at head_dim <= 128: both take
+// every other block of it, and the first takes the second's output in at the end (128 lists of 8192 keys, 20 to 32 rows:
+// head_dim 64 102 -> 74 us, 128 123 -> 115).
 //
 // The running maximum only moves when a row's scores exceed it by more than 2^8 (the weights then stay within fp32 and
 // bf16 range, and the sum, which uses the same maximum, cancels it): O is rescaled in tensor memory only then.
@@ -55,7 +57,8 @@ template <int D> struct Chunk {
     static constexpr int BARS = 2 * NSLOT + 18;
     static constexpr int TAIL_WALK = (BARS * 8 + 16 + 7) / 8 * 8;
     static constexpr int TAIL_STATS = TAIL_WALK + (int)sizeof(Walk);
-    static constexpr int TAIL = TAIL_STATS + (HALVES == 2 ? 2 * 2 * 128 * 4 : 0);      // [turn][half][row]
+    // two threads per row: [turn][half][row] maxima; two tiles: [row] maxima and sums of a split item
+    static constexpr int TAIL = TAIL_STATS + (HALVES == 2 ? 2 * 2 * 128 * 4 : 128 * 8);
     static constexpr int SMEM = 1024 + (int)(TILES * Q_TILE) + NSLOT * (int)SLOT + TAIL;
     static constexpr uint32_t O_COL = 256;              // tensor memory: S of tile t at 2 t BK, P of buffer b BK + b BK / 2 on, O from 256
     static_assert(SMEM + 256 <= 232448, "a CTA's shared memory, with room for static arrays");
@@ -263,75 +266,89 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         Ring k_ring = {0, 0}, v_ring = {(uint32_t)C::NK, 0};
         while (next_item(a, walk, C::ROWS, BK, it)) {
             const int count = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
-            const int nt = __shfl_sync(0xffffffffu, C::TILES == 2 && it.li.rows_tok * a.G - it.tile * C::ROWS > 128 ? 2 : 1, 0);
-            if (t >= nt) {                              // nothing to do with these blocks but to give their slots back
+            const bool split = __shfl_sync(0xffffffffu, C::TILES == 2 && it.li.rows_tok * a.G - it.tile * C::ROWS <= 128, 0);
+            const int mine = split ? (count + 1 - t) / 2 : count;      // blocks t, t + 2, .. or all of them
+            // blocks that the other warp works on: their slots are only given back
+            auto skip = [&](Ring& ring, int slots, int first, int end) {
 #pragma unroll 1
-                for (int i = 0; i < count; ++i) {
-                    for (int c = 0; c < C::KC; ++c) {
-                        if (ok) ok = mbar_wait<C::PAIR>(full(k_ring.slot), k_ring.phase, abort_flag);
-                        if (leader) mbar_arrive(empty(k_ring.slot));
-                        k_ring.next(0, C::NK);
-                    }
-                    for (int c = 0; c < C::VC; ++c) {
-                        if (ok) ok = mbar_wait<C::PAIR>(full(v_ring.slot), v_ring.phase, abort_flag);
-                        if (leader) mbar_arrive(empty(v_ring.slot));
-                        v_ring.next(C::NK, NS);
-                    }
+                for (int c = 0; c < slots; ++c) {
+                    if (ok) ok = mbar_wait<C::PAIR>(full(ring.slot), ring.phase, abort_flag);
+                    if (leader) mbar_arrive(empty(ring.slot));
+                    ring.next(first, end);
                 }
-                ok = __all_sync(0xffffffffu, ok);
-                continue;
-            }
-            if (ok) ok = mbar_wait<C::PAIR>(q_full(t), q_phase, abort_flag);
-            q_phase ^= 1;
+            };
+            // (two copies: what a split item adds would cost the others a few percent)
+            auto work = [&](auto is_split) {
+                constexpr bool SPLIT = decltype(is_split)::value;
+                if (SPLIT && mine == 0) {
+                    skip(k_ring, C::KC, 0, C::NK);
+                    skip(v_ring, C::VC, C::NK, NS);
+                    return;
+                }
+                if (ok) ok = mbar_wait<C::PAIR>(q_full(t), q_phase, abort_flag);
+                q_phase ^= 1;
 #pragma unroll 1
-            for (int j = -1; j < count; ++j) {
-                if (j + 1 < count) {                    // S = Q K(j + 1)^T, once the softmax has read the scores before
-                    if (j >= 0) {
-                        if (ok) ok = mbar_wait<C::PAIR>(s_read(t), r_phase, abort_flag);
-                        r_phase ^= 1;
-                    }
+                for (int j = -1; j < mine; ++j) {
+                    if (j + 1 < mine) {                     // S = Q K(j + 1)^T, once the softmax has read the scores before
+                        if (SPLIT) skip(k_ring, (j < 0 ? t : 1) * C::KC, 0, C::NK);
+                        if (j >= 0) {
+                            if (ok) ok = mbar_wait<C::PAIR>(s_read(t), r_phase, abort_flag);
+                            r_phase ^= 1;
+                        }
 #pragma unroll
-                    for (int c = 0; c < C::KC; ++c) {
-                        if (ok) ok = mbar_wait<C::PAIR>(full(k_ring.slot), k_ring.phase, abort_flag);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (ok) {
-                            tc_fence_after_sync();
-                            const uint64_t qd = q_desc + c * C::KW * (16384 >> 4), kd = k_desc + k_ring.slot * (C::SLOT >> 4);
+                        for (int c = 0; c < C::KC; ++c) {
+                            if (ok) ok = mbar_wait<C::PAIR>(full(k_ring.slot), k_ring.phase, abort_flag);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (ok) {
+                                tc_fence_after_sync();
+                                const uint64_t qd = q_desc + c * C::KW * (16384 >> 4), kd = k_desc + k_ring.slot * (C::SLOT >> 4);
 #pragma unroll
-                            for (int ks = 0; ks < 4 * C::KW; ++ks) {
-                                const uint64_t q_at = qd + (ks / 4) * (16384 >> 4) + ks % 4 * 2, k_at = kd + (ks / 4) * (C::KROWS * 128 >> 4) + ks % 4 * 2;
-                                if (C::PAIR) umma_bf16_pair_warp(leader, s_tmem, q_at, k_at, idesc_s, c + ks > 0 ? 1u : 0u);
-                                else umma_bf16_warp(leader, s_tmem, q_at, k_at, idesc_s, c + ks > 0 ? 1u : 0u);
+                                for (int ks = 0; ks < 4 * C::KW; ++ks) {
+                                    const uint64_t q_at = qd + (ks / 4) * (16384 >> 4) + ks % 4 * 2;
+                                    const uint64_t k_at = kd + (ks / 4) * (C::KROWS * 128 >> 4) + ks % 4 * 2;
+                                    if (C::PAIR) umma_bf16_pair_warp(leader, s_tmem, q_at, k_at, idesc_s, c + ks > 0 ? 1u : 0u);
+                                    else umma_bf16_warp(leader, s_tmem, q_at, k_at, idesc_s, c + ks > 0 ? 1u : 0u);
+                                }
+                                commit(empty(k_ring.slot));
                             }
-                            commit(empty(k_ring.slot));
+                            k_ring.next(0, C::NK);
                         }
-                        k_ring.next(0, C::NK);
+                        if (ok) commit(s_full(t));
                     }
-                    if (ok) commit(s_full(t));
-                }
-                if (j >= 0) {                           // O += P(j) V(j)
-                    const int b = j & 1;
-                    if (ok) ok = mbar_wait<C::PAIR>(p_full(t, b), (p_phase >> b) & 1, abort_flag);
-                    p_phase ^= 1u << b;
+                    if (j >= 0) {                           // O += P(j) V(j)
+                        const int b = j & 1;
+                        if (SPLIT) skip(v_ring, (j == 0 ? t : 1) * C::VC, C::NK, NS);
+                        if (ok) ok = mbar_wait<C::PAIR>(p_full(t, b), (p_phase >> b) & 1, abort_flag);
+                        p_phase ^= 1u << b;
 #pragma unroll
-                    for (int c = 0; c < C::VC; ++c) {
-                        if (ok) ok = mbar_wait<C::PAIR>(full(v_ring.slot), v_ring.phase, abort_flag);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (ok) {
-                            tc_fence_after_sync();
-                            const uint64_t vd = v_desc + v_ring.slot * (C::SLOT >> 4);
-                            const uint32_t p_tmem = s_tmem + BK + b * (BK / 2) + c * (C::VKEYS / 2);
+                        for (int c = 0; c < C::VC; ++c) {
+                            if (ok) ok = mbar_wait<C::PAIR>(full(v_ring.slot), v_ring.phase, abort_flag);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (ok) {
+                                tc_fence_after_sync();
+                                const uint64_t vd = v_desc + v_ring.slot * (C::SLOT >> 4);
+                                const uint32_t p_tmem = s_tmem + BK + b * (BK / 2) + c * (C::VKEYS / 2);
 #pragma unroll
-                            for (int ks = 0; ks < C::VKEYS / 16; ++ks)
-                                if (C::PAIR) umma_bf16_ts_pair_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
-                                else umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, c + ks > 0 ? 1u : (uint32_t)j);
-                            commit(empty(v_ring.slot));
+                                for (int ks = 0; ks < C::VKEYS / 16; ++ks) {
+                                    const uint32_t onto = c + ks > 0 ? 1u : (uint32_t)j;
+                                    if (C::PAIR) umma_bf16_ts_pair_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, onto);
+                                    else umma_bf16_ts_warp(leader, o_tmem, p_tmem + ks * 8, vd + v_step[ks], idesc_o, onto);
+                                }
+                                commit(empty(v_ring.slot));
+                            }
+                            v_ring.next(C::NK, NS);
                         }
-                        v_ring.next(C::NK, NS);
+                        if (ok) commit(o_done(t, b));
                     }
-                    if (ok) commit(o_done(t, b));
                 }
-            }
+                if (SPLIT && t + 2 * mine - 1 < count) {
+                    skip(k_ring, C::KC, 0, C::NK);
+                    skip(v_ring, C::VC, C::NK, NS);
+                }
+            };
+            if (C::TILES == 2 && split) work(std::true_type());
+            else work(std::false_type());
+            ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok) {                                      // MMAs in flight end before the tensor memory goes back
             commit(drained(t));
@@ -351,7 +368,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const uint32_t o_col = tmem + lanes + C::O_COL + t * D + half * OWN;
         float* stats = reinterpret_cast<float*>(tail + C::TAIL_STATS);
         const int vbox = min(1 << a.shift, C::VKEYS);   // keys of a V box
-        const int part_tile = C::PAIR ? rank : t;       // which 128 of a row tile's rows
         uint32_t s_phase = 0, turn = 0, tails = 0, uses[2] = {0, 0};   // uses: of the weights' buffers, before this item
         long long seq = 0;                              // V slots of the items before this one
         // the queries take the sign (exact), so that max(c S) = c max(S); a scale of zero becomes one that leaves nothing of
@@ -369,8 +385,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             const ListInfo& li = it.li;
             const int count = it.b1 - it.b0;
             const int live_rows = li.rows_tok * a.G - it.tile * C::ROWS;
-            const int nt = C::TILES == 2 && live_rows > 128 ? 2 : 1;
-            if (t >= nt) {
+            // Two row tiles and rows for one: they split the blocks, each with its own running maximum, sum and output.
+            const bool split = C::TILES == 2 && live_rows <= 128;
+            const int mine = split ? (count + 1 - t) / 2 : count;
+            const int part_tile = C::PAIR ? rank : split ? 0 : t;      // which 128 of a row tile's rows
+            if (mine == 0) {
                 seq += (long long)count * C::VC;
                 continue;
             }
@@ -419,113 +438,152 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 if (ok) ok = mbar_wait(o_done(t, j & 1), (uses[j & 1] + (uint32_t)(j >> 1)) & 1, abort_flag);
                 __syncwarp();
             };
-            for (int j = 0; j < count; ++j) {
-                const int key0 = (it.b0 + j) * BK, b = j & 1;
-                if (ok) ok = mbar_wait(s_full(t), s_phase, abort_flag);
-                s_phase ^= 1;
-                if (key0 + BK > li.n) {
-                    // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN: they become
-                    // zero before the weights let the product go (by both tiles: the zeros are the same).  (A parity tells two
-                    // neighbouring phases apart: the slots' earlier use is known to be over when the product before is.)
-                    if (C::PAIR) {
-                        if (ok) ok = mbar_wait(v_tail(tails), (tails >> 1) & 1, abort_flag);
-                        ++tails;
-                    } else if (j > 0) {
-                        wait_product(j - 1);
-                    }
-                    for (int c = 0; c < C::VC; ++c) {
-                        const long long at = seq + j * C::VC + c;
-                        const uint32_t s = C::NK + (uint32_t)(at % C::NV);
-                        const int from = max(0, li.n - key0 - c * C::VKEYS);
-                        if (from >= C::VKEYS) continue;
-                        if (!C::PAIR && ok) ok = mbar_wait(full(s), (uint32_t)(at / C::NV) & 1, abort_flag);
-                        constexpr int V_PIECES = C::VCH / 8;
-                        for (int i = tid; i < (C::VKEYS - from) * V_PIECES; i += TILE_THREADS) {
-                            const int r = from + i / V_PIECES, piece = i % V_PIECES;
-                            sts128(s_ring + s * C::SLOT + (r / vbox) * vbox * (C::VCH * 2) + ((piece / 8) * vbox + r % vbox) * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
-                        }
-                    }
-                    fence_proxy_async_smem();
-                }
-                __syncwarp();
-                tc_fence_after_sync();
-                const uint32_t s_col = tmem + lanes + 2 * t * BK;
-                uint32_t x[2][32];
-                tmem_ld_x32(s_col + half * 64, x[0]);
-                tmem_ld_x32(s_col + half * 64 + 32, x[1]);
-                tmem_ld_wait();                         // (of the whole warp)
-                tc_fence_before_sync();
-                if (lane == 0 && j + 1 < count) tell(s_read(t));
-                if (key0 + BK > seen) {
-                    const int local = lim - key0 - half * 64;
-#pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (i >= local) x[i / 32][i % 32] = 0xff800000u;
-                }
-                float top[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    top[i] = __uint_as_float(x[i / 2][i % 2 * 16]);
-#pragma unroll
-                    for (int e = 1; e < 15; e += 2)
-                        top[i] = max3(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + e]), __uint_as_float(x[i / 2][i % 2 * 16 + e + 1]));
-                    top[i] = fmaxf(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + 15]));
-                }
-                float raw = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                if (C::HALVES == 2) raw = fmaxf(raw, partner(raw));
-                const float m_blk = raw * scale;
-                const bool move = m_blk > m + kRescale; // (a row that has seen nothing has m = -infinity)
-                if (__any_sync(0xffffffffu, move)) {
-                    const float f = move ? ex2(m - m_blk) : 1.f;
-                    l *= f;
-                    if (move) m = m_blk;
-                    if (j > 0) {
-                        wait_product(j - 1);
-                        tc_fence_after_sync();
+            auto softmax = [&](auto is_split) {
+                constexpr bool SPLIT = decltype(is_split)::value;
 #pragma unroll 1
-                        for (int c = 0; c < OWN; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld_x32(o_col + c, o);
-                            tmem_ld_wait();
+                for (int j = 0; j < mine; ++j) {
+                    const int block = SPLIT ? 2 * j + t : j, key0 = (it.b0 + block) * BK, b = j & 1;
+                    if (ok) ok = mbar_wait(s_full(t), s_phase, abort_flag);
+                    s_phase ^= 1;
+                    if (key0 + BK > li.n) {
+                        // value rows behind the list's end hold anything, and a weight of zero does not silence a NaN: they become
+                        // zero before the weights let the product go (by both tiles: the zeros are the same).  (A parity tells two
+                        // neighbouring phases apart: the slots' earlier use is known to be over when the product before is.)
+                        if (C::PAIR) {
+                            if (ok) ok = mbar_wait(v_tail(tails), (tails >> 1) & 1, abort_flag);
+                            ++tails;
+                        } else if (j > 0) {
+                            wait_product(j - 1);
+                        }
+                        for (int c = 0; c < C::VC; ++c) {
+                            const long long at = seq + block * C::VC + c;
+                            const uint32_t s = C::NK + (uint32_t)(at % C::NV);
+                            const int from = max(0, li.n - key0 - c * C::VKEYS);
+                            if (from >= C::VKEYS) continue;
+                            if (!C::PAIR && ok) ok = mbar_wait(full(s), (uint32_t)(at / C::NV) & 1, abort_flag);
+                            constexpr int V_PIECES = C::VCH / 8;
+                            for (int i = tid; i < (C::VKEYS - from) * V_PIECES; i += TILE_THREADS) {
+                                const int r = from + i / V_PIECES, piece = i % V_PIECES;
+                                const uint32_t box = s_ring + s * C::SLOT + (r / vbox) * vbox * (C::VCH * 2);
+                                sts128(box + ((piece / 8) * vbox + r % vbox) * 128u + (piece % 8) * 16u, make_uint4(0, 0, 0, 0));
+                            }
+                        }
+                        fence_proxy_async_smem();
+                    }
+                    __syncwarp();
+                    tc_fence_after_sync();
+                    const uint32_t s_col = tmem + lanes + 2 * t * BK;
+                    uint32_t x[2][32];
+                    tmem_ld_x32(s_col + half * 64, x[0]);
+                    tmem_ld_x32(s_col + half * 64 + 32, x[1]);
+                    tmem_ld_wait();                         // (of the whole warp)
+                    tc_fence_before_sync();
+                    if (lane == 0 && j + 1 < mine) tell(s_read(t));
+                    if (key0 + BK > seen) {
+                        const int local = lim - key0 - half * 64;
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st_x32(o_col + c, o);
+                        for (int i = 0; i < 64; ++i)
+                            if (i >= local) x[i / 32][i % 32] = 0xff800000u;
+                    }
+                    float top[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        top[i] = __uint_as_float(x[i / 2][i % 2 * 16]);
+#pragma unroll
+                        for (int e = 1; e < 15; e += 2)
+                            top[i] = max3(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + e]), __uint_as_float(x[i / 2][i % 2 * 16 + e + 1]));
+                        top[i] = fmaxf(top[i], __uint_as_float(x[i / 2][i % 2 * 16 + 15]));
+                    }
+                    float raw = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    if (C::HALVES == 2) raw = fmaxf(raw, partner(raw));
+                    const float m_blk = raw * scale;
+                    const bool move = m_blk > m + kRescale; // (a row that has seen nothing has m = -infinity)
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float f = move ? ex2(m - m_blk) : 1.f;
+                        l *= f;
+                        if (move) m = m_blk;
+                        if (j > 0) {
+                            wait_product(j - 1);
+                            tc_fence_after_sync();
+#pragma unroll 1
+                            for (int c = 0; c < OWN; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld_x32(o_col + c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st_x32(o_col + c, o);
+                            }
                         }
                     }
-                }
-                // (the buffer that these weights go to is free: the scores of this block were issued, and so have ended, after
-                // the product of two blocks before)
-                // The two tiles take turns on the exponential unit (per scheduler: warps w and w + 4 are on the same one), so
-                // that the loads, maxima and waits of one run beside the exponentials of the other.
-                if (nt == 2 && (t == 1 || j > 0)) bar_sync(7 + t * 4 + quarter, 64);
-                const float z = m == -INFINITY ? 0.f : m;
-                const float2 c2 = make_float2(scale, scale), z2 = make_float2(-z, -z);
-                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    // (the buffer that these weights go to is free: the scores of this block were issued, and so have ended, after
+                    // the product of two blocks before)
+                    // The two tiles take turns on the exponential unit (per scheduler: warps w and w + 4 are on the same one), so
+                    // that the loads, maxima and waits of one run beside the exponentials of the other.
+                    if (C::TILES == 2 && !SPLIT && (t == 1 || j > 0)) bar_sync(7 + t * 4 + quarter, 64);
+                    const float z = m == -INFINITY ? 0.f : m;
+                    const float2 c2 = make_float2(scale, scale), z2 = make_float2(-z, -z);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t p[16];
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t p[16];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
-                        y.x = ex2(y.x);
-                        y.y = ex2(y.y);
-                        sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
-                        p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
+                        for (int e = 0; e < 32; e += 2) {
+                            float2 y = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), c2, z2);
+                            y.x = ex2(y.x);
+                            y.y = ex2(y.y);
+                            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
+                            p[e / 2] = pack_bf16(y.x, y.y);          // 8 significant bits per weight
+                        }
+                        tmem_st_x16(s_col + BK + b * (BK / 2) + half * 32 + i * 16, p);
                     }
-                    tmem_st_x16(s_col + BK + b * (BK / 2) + half * 32 + i * 16, p);
+                    if (C::TILES == 2 && !SPLIT && (t == 0 || j + 1 < mine)) bar_arrive(7 + (t ^ 1) * 4 + quarter, 64);
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    if (lane == 0) tell(p_full(t, b));
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 }
-                if (nt == 2 && (t == 0 || j + 1 < count)) bar_arrive(7 + (t ^ 1) * 4 + quarter, 64);
-                tmem_st_wait();
-                tc_fence_before_sync();
-                if (lane == 0) tell(p_full(t, b));
-                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-            }
+            };
+            if (C::TILES == 2 && split) softmax(std::true_type());
+            else softmax(std::false_type());
             // ---- output: with two threads per row each its channels
             if (C::HALVES == 2) l += partner(l);
-            wait_product(count - 1);
-            uses[0] += (uint32_t)(count + 1) / 2;
-            uses[1] += (uint32_t)count / 2;
+            wait_product(mine - 1);
+            uses[0] += (uint32_t)(mine + 1) / 2;
+            uses[1] += (uint32_t)mine / 2;
             tc_fence_after_sync();
+            if (split && count > 1) {
+                // the second tile's result into the first's (the warps w and w + 4 have the same lanes of tensor memory)
+                float2* st = reinterpret_cast<float2*>(stats) + row;
+                if (t == 1) {
+                    *st = make_float2(m, l);
+                    tc_fence_before_sync();
+                    bar_sync(1 + quarter, 64);
+                    bar_sync(1 + quarter, 64);          // read
+                    seq += (long long)count * C::VC;
+                    continue;
+                }
+                bar_sync(1 + quarter, 64);
+                tc_fence_after_sync();
+                const float2 y = *st;
+                const float m_new = fmaxf(m, y.x), z = m_new == -INFINITY ? 0.f : m_new;
+                const float f = ex2(m - z), fy = ex2(y.x - z);
+                m = m_new;
+                l = l * f + y.y * fy;
+#pragma unroll 1
+                for (int c = 0; c < OWN; c += 32) {
+                    uint32_t o[32], v[32];
+                    tmem_ld_x32(o_col + c, o);
+                    tmem_ld_x32(o_col + D + c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f + __uint_as_float(v[e]) * fy);
+                    tmem_st_x32(o_col + c, o);
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                bar_sync(1 + quarter, 64);
+            }
             // Rows leave in one piece through shared memory (where the queries were: every product with them has ended).
             auto stage = [&](int c, const float (&o)[32], float f) {
 #pragma unroll
@@ -655,7 +713,7 @@ ea_status launch(const ea_ctx* ctx, const ea_paged_shape& s, const AttnArgs& arg
     a.part_o = static_cast<float*>(ctx->workspace);
     a.part_ml = a.part_o + (size_t)C::PARTS * C::ROWS * D;
     CUtensorMap k_map, v_map;
-    const uint32_t kbox = s.page_rows < C::KROWS ? (uint32_t)s.page_rows : (uint32_t)C::KROWS, vbox = s.page_rows < C::VKEYS ? (uint32_t)s.page_rows : (uint32_t)C::VKEYS;
+    const uint32_t kbox = (uint32_t)(s.page_rows < C::KROWS ? s.page_rows : C::KROWS), vbox = (uint32_t)(s.page_rows < C::VKEYS ? s.page_rows : C::VKEYS);
     if (!ea_paged_map(ctx, s, k_pages, kbox, 1, &k_map) || !ea_paged_map(ctx, s, v_pages, vbox, C::VCH / 64, &v_map)) return EA_ERR_CUDA;
     auto kernel = paged_chunk_kernel<D>;
     static std::atomic<uint64_t> done{0};
