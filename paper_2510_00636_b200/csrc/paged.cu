@@ -21,9 +21,9 @@ namespace {
 //    13.3 (13.6 with three launches); beyond, the slots want all SMs: 131 072 slots 15.1 us against 13.5, 288 000 27.9
 //    against 19.0.  (A single CTA, without cluster barriers, is no faster for small plans: 10.2 us at 512 slots, 12.7
 //    against 10.5 at 8192.)
-//  * a plan without a slot map: one launch over all SMs, as nothing bounds the pages that move but the pool (288 lists
-//    taking 64 800 pages: 30 us for both calls against 38 in a cluster)
-//  * a slot map of standing tables: one launch over all SMs (8.4 us for 288 x 1000 slots with the launch)
+//  * a plan without a slot map: one launch over all SMs, as nothing bounds the pages that move but the pool (384 lists
+//    of up to 16 384 rows, a growth with its slots and this undoing: 30 us, 38 with the undoing in a cluster)
+//  * a slot map of standing tables: one launch over all SMs (288 lists of up to 8192 rows: 9 us with the launch)
 //  * more lists than a CTA keeps prefixes of: scan, pages and slots in three launches
 constexpr int kSelfScanLists = 4096;      // up to here every CTA scans the lengths itself (48 KiB of prefixes)
 constexpr int kScanSmem = 3 * (kSelfScanLists + 1) * 4;
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kMoveThreads) page_slots_kernel(const PlanArgs
 
 // rows <-> slots, 16 bytes of K and of V per thread and step.  A slot of -1 names no row; any other number outside the
 // pool is reported and skipped.  src: row i of the rows side begins at (i / group) * group_stride + (i % group) * d
-// elements (dense rows: group = 1, group_stride = d).  HBM: 2.7 GB of compacted rows into their slots 116 us, 0.91 of the
+// elements (dense rows: group = 1, group_stride = d).  HBM: 342 MB of compacted rows into their slots 116 us, 0.91 of the
 // measured copy rate; the rows of one token of one layer 1.9 us with the launch.
 template <bool STORE, int LPR /* 16-byte pieces per row */>
 __global__ void __launch_bounds__(256) page_rows_kernel(const int32_t* __restrict__ slots, long long n_rows, uint4* __restrict__ k_rows,

@@ -453,8 +453,8 @@ bool ea_paged_map(const ea_ctx* ctx, const ea_paged_shape& s, const void* pages,
 }
 
 // Up to 16 rows per list fit one tile of the kernel for few rows; more go to the tensor-core tiles of 128.  Both at 16 rows
-// of 128 lists of 8192 keys: head_dim 64 59 against 102 us, 128 100 against 121, 256 184 against 201; at 20 rows, where this
-// kernel reads everything twice: 184 against 121 at head_dim 128, 348 against 201 at 256.
+// of 128 lists of 8192 keys: head_dim 64 60 against 75 us, 128 101 against 115, 256 184 against 201; of 8 lists: 128 27 against
+// 42.  At 20 rows, where this kernel reads everything twice, 128 lists: 184 against 115 at head_dim 128, 348 against 201 at 256.
 static bool few_rows(int max_q, int G) { return (long long)max_q * G <= 16; }
 
 size_t ea_paged_attn_ws_bytes(const ea_paged_shape& s, int max_q) {
