@@ -641,7 +641,7 @@ ea_status ea_page_load(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* 
  * block_table, k_pages, v_pages  as above.  Rows behind a list's end may hold anything;
  *            value rows below it must be finite.  A page number outside the pool
  *            is recorded and leaves the outputs of its list unspecified.
- * scale      finite (1/sqrt(d) as a rule)
+ * scale      1/sqrt(d) as a rule; at most 2e38 in magnitude (EA_ERR_INVALID_ARG)
  * out        bf16 [n_tokens, Hq, d] dense, 16-byte aligned;  lse_opt fp32 [n_tokens, Hq] or NULL
  * Scores, softmax and sums are fp32; the weights are rounded to bf16 for the
  * product with V, whose accumulation is fp32.  The key blocks of the call are divided

@@ -25,7 +25,7 @@ namespace {
 // list ends, where they are merged in a fixed order.  At most 16 of the 128 rows of a tcgen05 tile would be in use here,
 // and the limit is memory: 32 sequences of up to 16 384 tokens, 28 heads on 4 lists of head_dim 128, 676 MB: 107 to 112 us
 // = 6.0 to 6.3 TB/s (0.94 to 0.98 of the measured copy rate); one sequence of 4096 tokens on 8 lists, 16.8 MB: 13 us, most of it
-// the latencies of the share's start, of seven blocks per CTA and of the join.
+// the latencies of the share's start, of four blocks per CTA and of the join.
 template <int D> struct Few {
     static constexpr int GROUPS = D == 256 ? 1 : 2;
     static constexpr int NW = 4 * GROUPS;
@@ -469,7 +469,7 @@ extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape
     if (!ctx) return EA_ERR_INVALID_ARG;
     ea_status st = ea_check_paged_shape(shape);
     if (st != EA_OK) return st;
-    if (n_tokens < 0 || max_q < 0 || max_q > n_tokens || !(fabsf(scale) <= 3.0e38f)) return EA_ERR_INVALID_ARG;
+    if (n_tokens < 0 || max_q < 0 || max_q > n_tokens || !(fabsf(scale) <= 2.0e38f)) return EA_ERR_INVALID_ARG;
     const int64_t dense = (int64_t)shape->n_q_heads * shape->head_dim;
     if (q_stride == 0) q_stride = dense;
     if (q_stride < dense || q_stride % 8 != 0) return EA_ERR_INVALID_ARG;

@@ -118,5 +118,13 @@ def test_attention_arguments(ea, ctx):
     assert L.ea_paged_attention(ctx, ref, *_vary(good, {2: 1 << 30, 4: 1}), None) == UNSUPPORTED
 
 
+def test_scales_whose_multiple_of_log2_e_overflows_are_refused(ea, ctx):
+    L, ref = ea.lib(), ctypes.byref(shape(ea))
+    good = [P, 0, 4, P, 2, P, P, P, P, 2.0e38, 1, P, P]
+    assert L.ea_paged_attention(ctx, ref, *good, None) == WORKSPACE
+    for scale in (2.5e38, -2.5e38):
+        assert L.ea_paged_attention(ctx, ref, *_vary(good, {9: scale}), None) == INVALID
+
+
 def test_status_string(ea):
     assert ea.lib().ea_status_string(7) == b"EA_ERR_PAGES"
