@@ -494,6 +494,25 @@ def test_on_another_stream_and_with_a_workspace_that_is_too_small(ea):
     assert e.value.status == 3
 
 
+@pytest.mark.parametrize("first,second", [(((28, 4, 128), 1), ((4, 2, 256), 70)), (((8, 2, 128), 40), ((4, 2, 64), 200))])
+def test_two_contexts_on_two_streams_do_not_disturb_each_other(ea, first, second):
+    caches = [make(ea, heads, 32, [m, m], [[4000, 1500][:heads[1]] * (heads[1] // 2), [m + 9] * heads[1]], seed=i)
+              for i, (heads, m) in enumerate((first, second))]
+    alone = [attend(ea, c, want_lse=True) for c in caches]
+    streams = [torch.cuda.Stream() for _ in caches]
+    torch.cuda.synchronize()
+    together = [[], []]
+    for _ in range(20):
+        for c, st, outs in zip(caches, streams, together):
+            with torch.cuda.stream(st):
+                outs.append(attend(ea, c, want_lse=True))
+    torch.cuda.synchronize()
+    for c, want, outs in zip(caches, alone, together):
+        c.ctx.sync_status()
+        for out, lse in outs:
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_binding_refuses_what_does_not_fit(ea):
     c = make(ea, (8, 2, 128), 16, [1, 1], [[20, 30], [40, 50]])
     args = dict(q=c.q, q_offsets=c.q_offsets, max_q=1, kv_lens=c.kv_lens, block_table=c.table, k_pages=c.k, v_pages=c.v)
