@@ -148,7 +148,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         const int box_rows = 1 << box_shift;
         const int subs = C::BK >> box_shift;
         const uint32_t leader = elect_one();
-        const uint64_t policy = evict_first_policy();                    // every row is read once: 142 -> 127 us for 676 MB
+        const uint64_t policy = evict_first_policy();                    // every row is read once (676 MB behind a write of all of L2: 142 -> 127 us)
         while (next_item(a, walk, 16, C::BK, it)) {
             const ListInfo& li = it.li;
             const int r = it.list, b0 = it.b0;

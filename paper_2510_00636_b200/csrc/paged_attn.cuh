@@ -185,7 +185,7 @@ constexpr int kPagedMaxCtas = 160;             // grid of the persistent kernels
 static_assert(2 * kPagedMaxCtas <= kCounters, "a counter per CTA and row tile");
 
 // The CTAs that share a row tile: `parts` of them from c0 on.  Each leaves its part (maxima, sums, unnormalised output)
-// in a slot of the workspace, and the one that arrives last joins them, in the order of the keys.  A CTA's first item
+// in a slot of the workspace; few rows: the one that arrives last joins all, in the order of the keys; chunks: in pairs.  A CTA's first item
 // is its slot 0, its last slot 1; only the tile's first CTA may have begun before the tile.  (Two tiles that are both
 // shared begin in different CTAs, so c0 names the counter of the arrivals.)
 struct Shared {

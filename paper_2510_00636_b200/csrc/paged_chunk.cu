@@ -26,7 +26,7 @@
 // query rows from shared memory for only 64 columns: 48 cycles an instruction where the arithmetic takes 32), the
 // exponentials 1024 of the special function units; the two tiles alternate on both and about 1600 pass.  2048 tokens
 // over 32 768 keys, 32 heads on 8 lists: 880 us = 1.21 PFLOP/s (0.72 of the measured cuBLAS rate); back to back, at the
-// clock that the power limit leaves, 1075 us (0.71 of the rate measured there).
+// clock that the power limit leaves, 1040 to 1070 us (0.71 to 0.74 of the rate measured there).
 #include <type_traits>
 
 #include "paged.h"
