@@ -642,6 +642,8 @@ ea_status ea_page_load(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* 
  *            value rows below it must be finite.  A page number outside the pool
  *            is recorded and leaves the outputs of its list unspecified.
  * scale      1/sqrt(d) as a rule; at most 2e38 in magnitude (EA_ERR_INVALID_ARG)
+ *            A token whose largest score scale * q . k is 7.4e8 (2^30 ln 2) or more in magnitude, or
+ *            NaN, gets NaN in out and lse: fp32 does not tell such scores' weights
  * out        bf16 [n_tokens, Hq, d] dense, 16-byte aligned;  lse_opt fp32 [n_tokens, Hq] or NULL
  * Scores, softmax and sums are fp32; the weights are rounded to bf16 for the
  * product with V, whose accumulation is fp32.  The key blocks of the call are divided

@@ -48,7 +48,7 @@ template <int D> struct Few {
 // Joins the parts of a tile of 16 rows, `live` of them in use: THREADS / 16 threads per row turn the parts' maxima and sums into
 // weights (in `weight`, [16][parts]), then every thread adds 4 channels of a row over the parts.
 template <int D, int THREADS>
-__device__ void join_parts(const AttnArgs& a, const Shared& sh, float* weight, int live, int row0, int q0, int head0) {
+__device__ void join_parts(const AttnArgs& a, const Shared& sh, const ListInfo& li, float* weight, int live, int row0, int head0) {
     constexpr int LANES = THREADS / 16, BATCH = D == 256 ? 8 : 16;
     {
         const int row = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -69,12 +69,11 @@ __device__ void join_parts(const AttnArgs& a, const Shared& sh, float* weight, i
 #pragma unroll
         for (int d = LANES / 2; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         if (row < live) {
+            const int tok = quotient(row0 + row, a.div_g);
+            l = sum_in_range(top, l, limit_of(li, a, tok));
             const float inv = inverse_sum(l);
             for (int p = lane; p < sh.parts; p += LANES) weight[row * kPagedMaxCtas + p] = ex2(weight[row * kPagedMaxCtas + p] - z) * inv;
-            if (lane == 0 && a.lse) {
-                const int tok = quotient(row0 + row, a.div_g);
-                a.lse[(size_t)(q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G] = lse_of(top, l);
-            }
+            if (lane == 0 && a.lse) a.lse[(size_t)(li.q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G] = lse_of(top, l);
         }
     }
     bar_sync(1, THREADS);
@@ -101,7 +100,7 @@ __device__ void join_parts(const AttnArgs& a, const Shared& sh, float* weight, i
             }
         }
         const int tok = quotient(row0 + row, a.div_g);
-        const size_t at = (size_t)(q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G;
+        const size_t at = (size_t)(li.q0 + tok) * a.Hq + head0 + row0 + row - tok * a.G;
         *reinterpret_cast<uint2*>(a.out + at * D + col) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
     }
 }
@@ -297,7 +296,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const float z = mx[x] == -INFINITY ? 0.f : mx[x];          // a row that has seen no key yet
-                        const float p0 = ex2(y[x][0] - z), p1 = ex2(y[x][1] - z), p2 = ex2(y[x][2] - z), p3 = ex2(y[x][3] - z);
+                        // (of the rounded products, all four alike, and not fused with them)
+                        const float p0 = ex2(__fsub_rn(y[x][0], z)), p1 = ex2(__fsub_rn(y[x][1], z));
+                        const float p2 = ex2(__fsub_rn(y[x][2], z)), p3 = ex2(__fsub_rn(y[x][3], z));
                         sum[x] += (p0 + p1) + (p2 + p3);
                         pf[x] = pack_bf16(p0, p1);           // the weights enter the product with 8 significant bits
                         pf[x + 2] = pack_bf16(p2, p3);
@@ -385,6 +386,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (!live[x]) continue;
+                    sum[x] = sum_in_range(mx[x], sum[x], lim[x]);
                     const float inv = inverse_sum(sum[x]);
                     const size_t row = (size_t)(li.q0 + tok[x]) * a.Hq + hd[x];
                     uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D) + t4;
@@ -411,7 +413,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             }
             bar_sync(1, C::NW * 32);
             if (*last_flag)
-                join_parts<D, C::NW * 32>(a, sh, merge, min(16, li.rows_tok * a.G - tile * 16), tile * 16, li.q0, head0);
+                join_parts<D, C::NW * 32>(a, sh, li, merge, min(16, li.rows_tok * a.G - tile * 16), tile * 16, head0);
         }
     }
     __syncthreads();

@@ -220,6 +220,11 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ float lse_of(float m, float l) {
     return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
+// The scores' magnitude in units of log 2 from which on a row is refused: what a product's rounding leaves, 2^-24 of it, would be
+// beyond what weights can hold (2^6 at this bound, the same in all weights of a row and in their sum).
+constexpr float kFar = 1073741824.0f;
+// The sum of a row that sees `seen` rows, or NaN (for its outputs too) where the largest of their scores is out of range.
+__device__ __forceinline__ float sum_in_range(float m, float l, int seen) { return seen > 0 && !(fabsf(m) < kFar) ? NAN : l; }
 // 1 / l for a row's normalisation: zero for a row that sees no key, NaN stays
 __device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }
 __device__ __forceinline__ float max3(float x, float y, float z) {

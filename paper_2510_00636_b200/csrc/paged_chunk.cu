@@ -499,9 +499,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                     const float m_blk = raw * scale;
                     const bool move = m_blk > m + kRescale; // (a row that has seen nothing has m = -infinity)
                     if (__any_sync(0xffffffffu, move)) {
-                        const float f = move ? ex2(m - m_blk) : 1.f;
+                        // (below the range the maximum stays at its end, and the weights of such scores are zero)
+                        const float m_new = move ? fmaxf(m_blk, -kFar) : m;
+                        const float f = move ? ex2(m - m_new) : 1.f;
                         l *= f;
-                        if (move) m = m_blk;
+                        m = m_new;
                         if (j > 0) {
                             wait_product(j - 1);
                             tc_fence_after_sync();
@@ -663,6 +665,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 }
             }
             if (write) {
+                l = sum_in_range(m, l, lim);
                 const float inv = inverse_sum(l);
 #pragma unroll 1
                 for (int c = 0; c < OWN; c += 32) {

@@ -1,0 +1,81 @@
+"""Paged cache at the edges of its range: scores beyond 32 bits, and what else a call may meet."""
+import math
+
+import pytest
+import torch
+
+import paged_reference as ref
+from test_gpu_paged import ea, i32          # noqa: F401 (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def one_hot_lists(ea, d, G, m, n, values, page=16, seed=0):
+    """One list of n rows whose scores are whole numbers: k = (x_p, 0, ..), q = (1 or -1, 0, ..), v whole."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    pages = ref.ceil_div(n, page)
+    shape = ea.make_paged_shape(1, G, 1, d, page, pages, pages)
+    ctx = ea.Context(0, ea.ea_paged_workspace_bytes(shape, m))
+    k, v = (torch.zeros(pages * page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k[:n, 0] = values(n, gen).to(torch.bfloat16)
+    v[:n] = torch.randint(-8, 9, (n, d), generator=gen, device="cuda").to(torch.bfloat16)
+    q = torch.zeros(m, G, d, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = torch.randint(0, 2, (m, G), generator=gen, device="cuda").to(torch.bfloat16) * 2 - 1
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, 1, pages)
+    return ctx, shape, q, i32([0, m]), m, i32([[n]]), table, k.view(pages, page, d), v.view(pages, page, d)
+
+
+ANY = lambda n, gen: torch.randint(-3, 4, (n,), generator=gen, device="cuda")                  # noqa: E731
+LOW = lambda n, gen: torch.randint(-5, -1, (n,), generator=gen, device="cuda")                 # noqa: E731
+CLIMB = lambda n, gen: torch.linspace(-100, 100, n, device="cuda").round()                     # noqa: E731
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 40), (2, 700), (3, 20000), (5, 40), (12, 700), (12, 20000), (70, 3), (70, 700), (70, 20000)])
+@pytest.mark.parametrize("values", [ANY, LOW, CLIMB], ids=["any", "low", "climb"])
+@pytest.mark.parametrize("scale", [2.0e38, -2.0e38, 1.0e38, -1.0e30, 3.0e9, 1.2e7, -6.0e6])
+def test_scores_out_of_range_are_not_answered_and_large_ones_pick_the_largest(ea, d, m, n, values, scale):      # noqa: F811
+    """A token whose largest score is 2^30 or more in units of log 2 gets NaN, in either kernel; below, scores that differ do so by
+    6e6 at least, and the rows of the largest one share the weight.
+
+    Whole numbers times `scale`.  The rows that share have one weight, 1 or (what the rounding of the largest score leaves) a
+    power of two that is rounded to bf16 for the product with V, 2^-8, and not for the sum; out's own rounding is 2^-8 (half a
+    step).  Sums of up to 20 000 weights, 16 at a time, and 160 parts: some 1400 roundings of 2^-24 of the mean of |v| at most.
+    lse carries six roundings of 2^-24 (two constants, three products, a sum) and that of the logarithm.
+    """
+    G = 4
+    args = one_hot_lists(ea, d, G, m, n, values)
+    ctx, q, k, v = args[0], args[2], args[7].view(-1, d)[:n], args[8].view(-1, d)[:n]
+    out, lse = ea.ea_paged_attention(*args, scale=scale, want_lse=True)
+    ctx.sync_status()
+    scale32 = torch.tensor(scale, dtype=torch.float32).double().item()
+    x = q[:, :, :1].double() * k[:, 0].double()                                                 # [m, G, n]
+    seen = torch.arange(n, device="cuda")[None] <= torch.arange(m, device="cuda")[:, None] + n - m
+    s = (scale32 * x).masked_fill(~seen[:, None], -INF)
+    best = s.amax(-1, keepdim=True)
+    hit = (s == best) & seen[:, None]
+    ties = hit.sum(-1)
+    far = (ties > 0) & (best[..., 0].abs() * math.log2(math.e) >= 2.0 ** 30)
+    assert bool(torch.isnan(out[far]).all()) and bool(torch.isnan(lse[far]).all())
+    want, mean = (torch.einsum("mgn,nd->mgd", hit.double(), x.double()) / ties.clamp(min=1)[..., None] for x in (v, v.abs()))
+    assert bool(((out.double() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -12 * mean)[~far].all())
+    blind = ties == 0
+    assert bool((lse[blind] == -INF).all()) and not bool(out[blind].any())
+    want_lse = best[..., 0] + torch.log(ties.double())
+    near = ~far & ~blind
+    err = (lse.double() - want_lse).abs()[near]
+    assert bool((err <= 2.0 ** -21 * want_lse[near].abs() + 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("m", [1, 40])
+def test_tokens_whose_scores_are_all_minus_infinity(ea, d, m):                                  # noqa: F811
+    """exp(-infinity) over a sum of zeros: not the zeros of a token that sees no row."""
+    args = one_hot_lists(ea, d, 4, m, 300, lambda n, gen: torch.full((n,), -INF, device="cuda"))
+    args[2][:, :, 0] = 1.0
+    args[7].view(-1, d)[:300, 1:] = 1.0
+    out, lse = ea.ea_paged_attention(*args, want_lse=True)
+    args[0].sync_status()
+    assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
