@@ -535,7 +535,8 @@ int64_t ea_n_floor(int64_t n_kept, double safeguard);
  * max_pages * page_rows <= 2^30; n_tokens * n_q_heads < 2^31.  The calls that use
  * the context's workspace need ea_paged_workspace_bytes (EA_ERR_WORKSPACE
  * otherwise).  They end the validity of a fused statistics operand
- * (ea_set_fused_stats), which lives there too.
+ * (ea_set_fused_stats), which lives there too; replayed in a graph, the scoring
+ * call that misses it records EA_ERR_INVALID_ARG.
  */
 typedef struct ea_paged_shape {
     int32_t n_seqs;      /* sequences in this call (or (layer, sequence) units)        */
@@ -686,7 +687,10 @@ ea_status ea_set_sm_budget(ea_ctx* ctx, int32_t n_sms);
  * statistics call of the context replaces the operand; a scoring call that is
  * given statistics (ea_score with sigma_bar, ea_score_wo, ea_score_q8) builds
  * its own operand in the same place, after which ea_score with NULL statistics
- * is refused until the next statistics call.
+ * is refused until the next statistics call.  The refusal is the host's: where such a
+ * call, or one of the paged cache, is repeated by a replayed graph between the two,
+ * the scoring call is not refused; its scores are then unspecified, and it
+ * records EA_ERR_INVALID_ARG (ea_sync_status).
  */
 ea_status ea_set_fused_stats(ea_ctx* ctx, int32_t on);
 
@@ -707,8 +711,9 @@ ea_status ea_set_side_sms(ea_ctx* ctx, int32_t n_sms);
 
 /*
  * Synchronises cuda_stream and returns the device-side status recorded since
- * the last call of this function (EA_OK, EA_ERR_DEVICE_TIMEOUT, EA_ERR_PAGES, or
- * EA_ERR_CUDA if the stream reports an error), then clears it.
+ * the last call of this function (EA_OK, EA_ERR_DEVICE_TIMEOUT, EA_ERR_PAGES,
+ * EA_ERR_INVALID_ARG (a scoring call whose fused operand was overwritten by a
+ * replayed graph), or EA_ERR_CUDA if the stream reports an error), then clears it.
  */
 ea_status ea_sync_status(ea_ctx* ctx, void* cuda_stream);
 

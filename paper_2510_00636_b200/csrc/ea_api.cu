@@ -145,8 +145,8 @@ ea_status ea_create(ea_ctx** out_ctx, int device, size_t workspace_bytes) {
     ctx->ev_stop = new (std::nothrow) cudaEvent_t[kMaxProfileEvents];
     bool ok = ctx->ev_start && ctx->ev_stop;
     if (ok && workspace_bytes > 0) ok = cudaMalloc(&ctx->workspace, workspace_bytes) == cudaSuccess;
-    if (ok) ok = cudaMalloc((void**)&ctx->counters, kCounters * sizeof(unsigned)) == cudaSuccess;
-    if (ok) ok = cudaMemset(ctx->counters, 0, kCounters * sizeof(unsigned)) == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
+    if (ok) ok = cudaMalloc((void**)&ctx->counters, (kCounters + 1) * sizeof(unsigned)) == cudaSuccess;
+    if (ok) ok = cudaMemset(ctx->counters, 0, (kCounters + 1) * sizeof(unsigned)) == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
     if (ok) ok = cudaHostAlloc((void**)&ctx->status_host, 2 * sizeof(int), cudaHostAllocMapped) == cudaSuccess;
     if (ok) {
         ctx->status_host[0] = ctx->status_host[1] = 0;
@@ -320,7 +320,7 @@ static ea_status score_impl(ea_ctx* ctx, const ea_shape* shape, const void* k, c
         if (st == EA_OK)
             st = ea_launch_logits_mma(ctx, *shape, kb, eq7, ws + plan.image,
                                       reinterpret_cast<float*>(ws + plan.vec), logits, lse_part, &n_chunks, stream);
-        if (st == EA_OK) st = ea_launch_lse_combine(ctx, *shape, lse_part, n_chunks, lse, stream);
+        if (st == EA_OK) st = ea_launch_lse_combine(ctx, *shape, lse_part, n_chunks, lse, stream, from_image);
         if (side) {
             // always rejoin, whatever happened in between: the caller's stream must not run ahead of the side pass
             EA_CUDA_TRY(cudaStreamWaitEvent(stream, ctx->ev_join, 0));

@@ -24,10 +24,12 @@ struct ea_ctx {
     void* workspace;
     size_t workspace_bytes;
     int* status_host;    // two pinned, mapped words: [0] device kernels write EA_ERR_DEVICE_TIMEOUT (other waits
-                         // give up when they see it), [1] the paged-cache calls write EA_ERR_PAGES
+                         // give up when they see it), [1] the paged-cache calls write EA_ERR_PAGES, and scoring calls
+                         // that find their fused operand overwritten EA_ERR_INVALID_ARG
     int* status_dev;     // device alias of status_host
     unsigned* counters;  // kCounters device words, zero between calls: arrivals at row tiles that several CTAs share
-                         // (ea_paged_attention; whoever is last puts its word back to zero)
+                         // (ea_paged_attention; whoever is last puts its word back to zero), the last one at page_resize_kernel;
+                         // behind them the operand word
     // benchmark instrumentation (ea_profile_begin / ea_profile_end)
     bool profiling;
     long long launches;          // kernels launched since ea_profile_begin
@@ -43,6 +45,10 @@ struct ea_ctx {
 
 constexpr int kMaxProfileEvents = 4096;
 constexpr int kCounters = 512;
+
+// Not zero while the workspace holds the images that the last fused statistics kernel wrote.  `image_ready` says so of the calls;
+// this word, written by the kernels, also of calls that a replayed graph repeats.
+static inline unsigned* ea_operand_word(const ea_ctx* ctx) { return ctx->counters + kCounters; }
 
 // Count `n` kernel launches made on behalf of `ctx`.
 static inline void ea_count_launches(const ea_ctx* ctx, int n) {
@@ -160,9 +166,10 @@ bool ea_mma_q8_supported(const ea_shape& s);
 ea_status ea_launch_logits_mma_q8(const ea_ctx* ctx, const ea_shape& s, const uint8_t* k_q8,
                                   const ea_quad_form& form, void* image, float* vec, float* logits,
                                   float* lse_part, int* n_chunks, cudaStream_t st);
-// log-sum-exp per softmax row from the per-work-unit partials of the tensor-core kernel
+// log-sum-exp per softmax row from the per-work-unit partials of the tensor-core kernel; from_image: the log-scores
+// were computed from a fused operand, and it is recorded if that was not there
 ea_status ea_launch_lse_combine(const ea_ctx* ctx, const ea_shape& s, const float* lse_part, int n_chunks,
-                                float* lse, cudaStream_t st);
+                                float* lse, cudaStream_t st, bool from_image = false);
 
 // ||v|| of every value row on n_ctas SMs (bulk-copy-fed stream), and the weighting that uses them.
 ea_status ea_launch_vnorm(const ea_ctx* ctx, const ea_shape& s, const __nv_bfloat16* v, int n_ctas, float* vnorm,

@@ -340,9 +340,11 @@ wo_gram_kernel(const __nv_bfloat16* __restrict__ w_o, int d_model, int Hq, int d
 }
 
 // One thread per softmax row: combine the (max, sum of exp) partials of its work units in order.
+// `operand` is given where the log-scores came from a fused operand.
 __global__ void lse_combine_kernel(const float* __restrict__ lse_part, int n_rows, int n_chunks,
-                                   float* __restrict__ lse) {
+                                   float* __restrict__ lse, const unsigned* operand, int* status) {
     const int r = blockIdx.x * blockDim.x + threadIdx.x;
+    if (operand && r == 0 && *operand == 0) status[1] = (int)EA_ERR_INVALID_ARG;
     if (r >= n_rows) return;
     const float* pp = lse_part + (size_t)r * n_chunks * 2;
     float m = -INFINITY, l = 0.f;
@@ -461,9 +463,10 @@ ea_status ea_launch_vnorm_rows(const ea_ctx* ctx, const ea_shape& s, const __nv_
 }
 
 ea_status ea_launch_lse_combine(const ea_ctx* ctx, const ea_shape& s, const float* lse_part, int n_chunks,
-                                float* lse, cudaStream_t st) {
+                                float* lse, cudaStream_t st, bool from_image) {
     const int rows = s.n_units * s.n_q_heads;
-    lse_combine_kernel<<<(rows + 127) / 128, 128, 0, st>>>(lse_part, rows, n_chunks, lse);
+    lse_combine_kernel<<<(rows + 127) / 128, 128, 0, st>>>(lse_part, rows, n_chunks, lse,
+                                                           from_image ? ea_operand_word(ctx) : nullptr, ctx->status_dev);
     ea_count_launches(ctx, 1);
     return EA_CHECK_LAUNCH();
 }

@@ -40,6 +40,7 @@ struct PlanArgs {
     int32_t* offsets;
     int32_t* scratch;            // prefixes of more than kSelfScanLists lists, and the totals
     unsigned* counter;           // arrivals of page_resize_kernel, zero between calls
+    unsigned* operand;           // the scratch lies where a fused statistics operand would
     int* status;                 // [1]: page status word
     int lists, Hkv, shift, n_pages, max_pages, by_token, slot_capacity;
     FastDiv div_hkv;             // by Hkv
@@ -264,7 +265,10 @@ __global__ void __launch_bounds__(kMoveThreads) page_resize_kernel(const PlanArg
 __global__ void __launch_bounds__(kScanThreads) page_scan_kernel(const PlanArgs a) {
     int32_t *take = a.scratch, *give = take + a.lists + 1, *rows = give + a.lists + 1;
     const Totals tot = scan_lists<kScanThreads>(a, take, give, rows);
-    if (threadIdx.x == 0) *reinterpret_cast<Totals*>(rows + a.lists + 1) = tot;
+    if (threadIdx.x == 0) {
+        *reinterpret_cast<Totals*>(rows + a.lists + 1) = tot;
+        *a.operand = 0;
+    }
     write_offsets(a, tot, rows);
 }
 
@@ -431,6 +435,7 @@ ea_status plan_call(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old
     a.scratch = static_cast<int32_t*>(ctx->workspace);
     a.status = ctx->status_dev;
     a.counter = ctx->counters + kCounters - 1;
+    a.operand = ea_operand_word(ctx);
     a.lists = (int)lists;
     a.Hkv = shape->n_kv_heads;
     a.div_hkv = fast_div(a.Hkv);

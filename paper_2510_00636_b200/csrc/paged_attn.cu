@@ -418,6 +418,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     }
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
+    if (threadIdx.x == 0 && blockIdx.x == 0) *a.operand = 0;
 }
 
 size_t few_part_floats(int d) { return (size_t)2 * kPagedMaxCtas * 16 * (d + 2); }
@@ -493,6 +494,7 @@ extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape
     a.lse = lse_opt;
     a.status = ctx->status_dev;
     a.counters = ctx->counters;
+    a.operand = ea_operand_word(ctx);
     a.lists = shape->n_seqs * shape->n_kv_heads;
     a.Hq = shape->n_q_heads;
     a.Hkv = shape->n_kv_heads;

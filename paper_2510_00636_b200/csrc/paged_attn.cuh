@@ -19,6 +19,7 @@ struct AttnArgs {
     float* part_o;               // unnormalised partial outputs, two row tiles per CTA
     float* part_ml;              // their maxima (of scores in units of log 2) and sums
     unsigned* counters;          // arrivals at the row tiles that several CTAs share
+    unsigned* operand;           // the parts lie where a fused statistics operand would
     int* status;
     int lists, Hq, Hkv, G, shift, n_pages, max_pages, n_tokens, max_q, causal;
     FastDiv div_g, div_hkv;      // by G and by Hkv

@@ -706,6 +706,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         else tmem_dealloc(tmem, 512);
     }
     if (threadIdx.x == 0 && *abort_flag) a.status[0] = (int)EA_ERR_DEVICE_TIMEOUT;
+    if (threadIdx.x == 0 && blockIdx.x == 0) *a.operand = 0;
 }
 
 template <int D>

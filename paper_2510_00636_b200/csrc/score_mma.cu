@@ -118,9 +118,10 @@ struct MmaParams {
 template <int D>
 __global__ void __launch_bounds__(256)
 sigma_image_kernel(const ea_quad_form form, int Hq, int Hkv, uint8_t* __restrict__ image,
-                   float* __restrict__ vec) {
+                   float* __restrict__ vec, unsigned* operand) {
     using G = Geo<D, true>;
     const int uh = blockIdx.x;
+    if (uh == 0 && threadIdx.x == 0) *operand = 0;           // a fused operand lay here
     const int u = uh / Hq, h = uh % Hq;
     const int Gq = Hq / Hkv;
     const int g = h / Gq, hg = h % Gq;
@@ -814,7 +815,7 @@ ea_status launch_mma(const ea_ctx* ctx, const ea_shape& s, const void* k, const 
     if (!make_k_map(&k_map, k, D, s.n_keys, ea_kv_cap(s), (long long)s.n_units * s.n_kv_heads, Q8)) return EA_ERR_CUDA;
 
     if (form.quad)
-        sigma_image_kernel<D><<<s.n_units * s.n_q_heads, 256, 0, st>>>(form, s.n_q_heads, s.n_kv_heads, image, vec);
+        sigma_image_kernel<D><<<s.n_units * s.n_q_heads, 256, 0, st>>>(form, s.n_q_heads, s.n_kv_heads, image, vec, ea_operand_word(ctx));
     auto kern = logits_mma_kernel<D, PAIR, Q8>;
     EA_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
     const long long want = (long long)p.n_groups * p.n_subsets;

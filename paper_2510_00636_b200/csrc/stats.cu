@@ -85,6 +85,7 @@ struct StatsImage {
     int Hkv;
     float lin_scale;     // 1 / sqrt(d)
     float quad_scale;    // 1 / (2 d)
+    unsigned* operand;   // set once the images are there (to whatever runs after this kernel)
 };
 
 // Shared memory: the staged chunk (hi and lo, kKC rows of the block's channels, padded by 16 bytes so that
@@ -427,6 +428,7 @@ stats_mma_kernel(const QT* __restrict__ q_win, const float* __restrict__ coef, i
         if (img.image) {
             // ---- the covariance image of this head, bit for bit what sigma_image_kernel builds from sigma_bar
             using L = EaImage<D>;
+            if (uh == 0 && tid == 0) *img.operand = 1;
             const int h = uh % Hq, Gq = Hq / img.Hkv;
             const int g = h / Gq, hg = h % Gq;
             const int n_subsets = (Gq + L::HPC - 1) / L::HPC;
@@ -506,7 +508,8 @@ static ea_status launch_stats(const ea_ctx* ctx, const ea_shape& s, const QT* q_
     const float inv_norm =
         1.0f / (float)(s.cov_norm == EA_COV_SAMPLE ? s.window - 1 : s.window);
     const unsigned heads = (unsigned)(s.n_units * s.n_q_heads);
-    const StatsImage img = {static_cast<uint8_t*>(image), vec, s.n_kv_heads, 1.0f / sqrtf((float)d), 0.5f / (float)d};
+    const StatsImage img = {static_cast<uint8_t*>(image), vec, s.n_kv_heads, 1.0f / sqrtf((float)d), 0.5f / (float)d,
+                            ctx ? ea_operand_word(ctx) : nullptr};
     int n_launches = 2;
     auto launch = [&](auto kern, int smem, unsigned blocks_y) {
         if (smem > 48 * 1024 &&

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paged_reference as ref
-from test_gpu_paged import ea, i32          # noqa: F401 (a fixture)
+from test_gpu_paged import Cache, attend, ea, i32, make          # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +79,52 @@ def test_tokens_whose_scores_are_all_minus_infinity(ea, d, m):                  
     out, lse = ea.ea_paged_attention(*args, want_lse=True)
     args[0].sync_status()
     assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+
+
+@pytest.mark.parametrize("which", ["few rows", "chunk", "plan", "score"])
+def test_a_replay_that_overwrites_a_fused_operand_is_recorded(ea, which):                       # noqa: F811
+    """The operand of fused statistics lies where paged calls, and scoring calls with statistics, put theirs; the host sees no replay."""
+    S, Hq, Hkv, d, n, W = 1, 8, 2, 128, 256, 32
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn(*x, generator=gen, device="cuda").to(torch.bfloat16) for x in ((S, Hq, W, d), (S, Hkv, n, d), (S, Hkv, n, d)))
+    dense = ea.make_shape(S, Hq, Hkv, d, n, W)
+    if which == "plan":
+        c = Cache(ea, 5000, 1, 1, 64, 16, 5000, 1)
+        lens = [c.lens([0] * 5000), c.lens([9] * 5000)]
+        slots, offsets = torch.empty(45000, dtype=torch.int32, device="cuda"), torch.empty(5001, dtype=torch.int32, device="cuda")
+    else:
+        c = make(ea, (8, 2, 128), 16, [40 if which == "chunk" else 1], [[2000, 3000]])
+    ctx = ea.Context(0, max(ea.ea_workspace_bytes(dense), ea.ea_paged_workspace_bytes(c.shape, 40)))
+    c.ctx = ctx
+    pos = torch.full((S,), n, dtype=torch.int64, device="cuda")
+    given = ea.ea_query_stats(ctx, dense, q, pos, 64, 1e6)
+
+    def call():
+        if which == "plan":
+            ea.ea_page_plan(ctx, c.shape, *lens, c.table, c.free, c.n_free, slots=slots, offsets=offsets)
+        elif which == "score":
+            ea.ea_score(ctx, dense, k, v, *given, 0.02)
+        else:
+            attend(ea, c)
+
+    graph = torch.cuda.CUDAGraph()
+    if which != "plan":
+        call()
+    with torch.cuda.graph(graph):
+        call()
+    ctx.set_fused_stats(True)
+    for _ in range(2):
+        ea.ea_query_stats(ctx, dense, q, pos, 64, 1e6)
+        for _ in range(2):
+            scores = ea.ea_score(ctx, dense, k, v, None, None, 0.02)
+        ctx.sync_status()
+        ea.ea_query_stats(ctx, dense, q, pos, 64, 1e6)
+        graph.replay()
+        ea.ea_score(ctx, dense, k, v, None, None, 0.02)
+        with pytest.raises(ea.EAError) as e:
+            ctx.sync_status()
+        # (the second plan finds an empty pool and records that; either word is an error)
+        assert e.value.status in ((1, 7) if which == "plan" else (1,))
+        ctx.sync_status()
+    assert torch.equal(scores, ea.ea_score(ctx, dense, k, v, *given, 0.02))
+    ctx.sync_status()
