@@ -574,7 +574,9 @@ ea_status ea_paged_workspace_bytes(const ea_paged_shape* shape, int32_t max_q, s
  * free_pages   int32 [n_pages], n_free int32 [1]: the first n_free entries are
  *              the pages that nobody holds; both updated
  * slots_opt    int32 [slot_capacity] or NULL: the slots of the rows old .. new - 1 of
- *              every list that grows, in the given order; -1 behind the last
+ *              every list that grows, in the given order; -1 behind the last.  NULL (with
+ *              slot_capacity 0) asks for no slots; a map of capacity 0 that is not
+ *              NULL holds no row, so that no list may grow
  * offsets_opt  NULL, or int32 [n_seqs * Hkv + 1] (by list): where each list's
  *              slots begin; int32 [n_seqs + 1] (by token): each sequence's first
  *              token, the q_offsets of ea_paged_attention

@@ -692,7 +692,10 @@ def _slot_map(shape, order, n_slots, slots, offsets, device, like):
         raise ValueError("slots: expected one dimension")
     if offsets is None:
         offsets = like.new_empty((n,))
-    return slots, offsets, _address(slots, torch.int32, None, device, "slots"), _address(offsets, torch.int32, (n,), device, "offsets")
+    a_slots = _address(slots, torch.int32, None, device, "slots")
+    a_off = _address(offsets, torch.int32, (n,), device, "offsets")
+    # an empty map has no address, and none would mean that no map is asked for: any address does, as none of it is written
+    return slots, offsets, a_slots or a_off, a_off
 
 
 def ea_page_plan(ctx: Context, shape: PagedShape, old_lens, new_lens, block_table, free_pages, n_free, n_slots=None,

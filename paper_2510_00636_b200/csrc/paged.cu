@@ -368,7 +368,7 @@ ea_status launch_plan(const ea_ctx* ctx, PlanArgs a, cudaStream_t st) {
         ea_count_launches(ctx, 1);
         return EA_CHECK_LAUNCH();
     }
-    if (few && !a.slots) {
+    if (few && a.slot_capacity == 0) {
         // nothing bounds the pages that move but the pool
         static std::atomic<uint64_t> done{0};
         const ea_status err = ea_allow_smem(page_resize_kernel, kScanSmem, ctx->device, done);
@@ -403,8 +403,8 @@ ea_status launch_plan(const ea_ctx* ctx, PlanArgs a, cudaStream_t st) {
         const long long pages = (a.n_pages + kMoveThreads - 1) / kMoveThreads, most = (long long)ctx->sm_count * 4;
         page_move_kernel<<<(unsigned)(pages < 1 ? 1 : pages < most ? pages : most), kMoveThreads, 0, st>>>(a);
     }
-    if (a.slots) page_slots_kernel<false><<<slot_grid, kMoveThreads, 0, st>>>(a);
-    ea_count_launches(ctx, 1 + (resize ? 1 : 0) + (a.slots ? 1 : 0));
+    if (a.slot_capacity > 0) page_slots_kernel<false><<<slot_grid, kMoveThreads, 0, st>>>(a);
+    ea_count_launches(ctx, 1 + (resize ? 1 : 0) + (a.slot_capacity > 0 ? 1 : 0));
     return EA_CHECK_LAUNCH();
 }
 

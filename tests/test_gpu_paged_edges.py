@@ -128,3 +128,27 @@ def test_a_replay_that_overwrites_a_fused_operand_is_recorded(ea, which):       
         ctx.sync_status()
     assert torch.equal(scores, ea.ea_score(ctx, dense, k, v, *given, 0.02))
     ctx.sync_status()
+
+
+@pytest.mark.parametrize("lists", [4, 5000])
+@pytest.mark.parametrize("given", [False, True])
+def test_an_empty_slot_map_holds_no_rows(ea, lists, given):                                     # noqa: F811
+    c = Cache(ea, lists // 2, 2, 2, 64, 16, 2 * lists, 8)
+    kw = dict(slots=i32([])) if given else dict(n_slots=0)
+    before = [x.clone() for x in (c.table, c.free, c.n_free)]
+    none, some = [0] * lists, [0] * (lists - 1) + [17]
+    for refused in (lambda: c.plan(none, some, **kw),
+                    lambda: ea.ea_page_slots(c.ctx, c.shape, c.table, c.lens(none), c.lens(some), **kw)):
+        slots, offsets = refused()
+        with pytest.raises(ea.EAError) as e:
+            c.ctx.sync_status()
+        assert e.value.status == 7 and slots.numel() == 0 and not bool(offsets.any())
+        assert all(torch.equal(a, b) for a, b in zip(before, (c.table, c.free, c.n_free)))
+    assert c.plan(none, some) is None                       # without a map they grow
+    c.py.resize(none, some)
+    c.same()
+    c.plan(some, none, **kw)                                # and shrink with an empty one
+    c.py.resize(some, none)
+    c.same()
+    ea.ea_page_slots(c.ctx, c.shape, c.table, c.lens(some), c.lens(none), **kw)
+    c.ctx.sync_status()
