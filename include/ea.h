@@ -534,7 +534,8 @@ int64_t ea_n_floor(int64_t n_kept, double safeguard);
  * 128 or 256; n_seqs * n_kv_heads <= 65535; n_pages * page_rows < 2^31;
  * max_pages * page_rows <= 2^30; n_tokens * n_q_heads < 2^31.  The calls that use
  * the context's workspace need ea_paged_workspace_bytes (EA_ERR_WORKSPACE
- * otherwise).  They end the validity of a fused statistics operand
+ * otherwise).  What a call of this section writes may overlap none of its other
+ * buffers (EA_ERR_INVALID_ARG).  They end the validity of a fused statistics operand
  * (ea_set_fused_stats), which lives there too; replayed in a graph, the scoring
  * call that misses it records EA_ERR_INVALID_ARG.
  */

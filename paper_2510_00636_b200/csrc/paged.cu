@@ -424,6 +424,12 @@ ea_status plan_call(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* old
         return EA_ERR_INVALID_ARG;
     if (ctx->workspace_bytes < scan_bytes(*shape)) return EA_ERR_WORKSPACE;
     if (lists == 0 && slot_capacity == 0 && !offsets) return EA_OK;
+    const long long i32 = sizeof(int32_t);
+    const Span spans[] = {{old_lens, lists * i32, false}, {new_lens, lists * i32, false},
+                          {table, lists * shape->max_pages * i32, resize}, {free_pages, resize ? shape->n_pages * i32 : 0, true},
+                          {n_free, resize ? i32 : 0, true}, {slots, slot_capacity * i32, true},
+                          {offsets, (order == EA_SLOTS_BY_TOKEN ? shape->n_seqs + 1LL : lists + 1) * i32, true}};
+    if (outputs_overlap(spans)) return EA_ERR_INVALID_ARG;
     PlanArgs a = {};
     a.old_lens = old_lens;
     a.new_lens = new_lens;
@@ -472,6 +478,11 @@ ea_status rows_call(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* slo
     if (n_rows == 0) return EA_OK;
     if (!slots || !k_rows || !v_rows || (shape->n_pages > 0 && (!k_pages || !v_pages))) return EA_ERR_INVALID_ARG;
     if (!aligned4(slots) || !aligned16(k_rows) || !aligned16(v_rows) || !aligned16(k_pages) || !aligned16(v_pages)) return EA_ERR_INVALID_ARG;
+    const long long groups = n_rows / shape->n_kv_heads, pool = (long long)shape->n_pages * shape->page_rows * d * 2;
+    auto rows_bytes = [&](int64_t stride) { return 2 * (strided && stride ? (groups - 1) * stride + dense : n_rows * d); };
+    const Span spans[] = {{slots, n_rows * 4, false}, {k_rows, rows_bytes(k_stride), !STORE}, {v_rows, rows_bytes(v_stride), !STORE},
+                          {k_pages, pool, STORE}, {v_pages, pool, STORE}};
+    if (outputs_overlap(spans)) return EA_ERR_INVALID_ARG;
     int prev = 0;
     EA_CUDA_TRY(cudaGetDevice(&prev));
     if (prev != ctx->device) EA_CUDA_TRY(cudaSetDevice(ctx->device));

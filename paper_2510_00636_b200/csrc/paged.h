@@ -38,6 +38,24 @@ static inline ea_status ea_allow_smem(Kernel kernel, int bytes, int device, std:
     return EA_OK;
 }
 
+// A buffer of a call.  Kernels read inputs in any order beside their writes, so that an output may overlap nothing else.
+struct Span {
+    const void* at;
+    long long bytes;
+    bool output;
+};
+template <int N>
+static inline bool outputs_overlap(const Span (&spans)[N]) {
+    for (int i = 0; i < N; ++i)
+        for (int j = 0; j < i; ++j) {
+            const uintptr_t a = reinterpret_cast<uintptr_t>(spans[i].at), b = reinterpret_cast<uintptr_t>(spans[j].at);
+            if ((spans[i].output || spans[j].output) && a && b && spans[i].bytes > 0 && spans[j].bytes > 0 &&
+                a < b + (unsigned long long)spans[j].bytes && b < a + (unsigned long long)spans[i].bytes)
+                return true;
+        }
+    return false;
+}
+
 ea_status ea_check_paged_shape(const ea_paged_shape* s);
 // Workspace of ea_paged_attention (partial results of lists that several CTAs share).
 size_t ea_paged_attn_ws_bytes(const ea_paged_shape& s, int max_q);

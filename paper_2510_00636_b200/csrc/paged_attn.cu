@@ -484,6 +484,13 @@ extern "C" ea_status ea_paged_attention(ea_ctx* ctx, const ea_paged_shape* shape
         !aligned4(block_table) || !aligned4(lse_opt))
         return EA_ERR_INVALID_ARG;
     if (ctx->workspace_bytes < ea_paged_attn_ws_bytes(*shape, max_q)) return EA_ERR_WORKSPACE;
+    const long long lists = (long long)shape->n_seqs * shape->n_kv_heads;
+    const long long pool = (long long)shape->n_pages * shape->page_rows * shape->head_dim * 2;
+    const Span spans[] = {{q, 2 * ((n_tokens - 1) * q_stride + dense), false}, {q_offsets, (shape->n_seqs + 1LL) * 4, false},
+                          {kv_lens, lists * 4, false}, {block_table, lists * shape->max_pages * 4, false}, {k_pages, pool, false},
+                          {v_pages, pool, false}, {out, 2 * n_tokens * dense, true},
+                          {lse_opt, 4LL * n_tokens * shape->n_q_heads, true}};
+    if (outputs_overlap(spans)) return EA_ERR_INVALID_ARG;
     AttnArgs a = {};
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.q_stride = q_stride;

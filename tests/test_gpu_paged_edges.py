@@ -152,3 +152,41 @@ def test_an_empty_slot_map_holds_no_rows(ea, lists, given):                     
     c.same()
     ea.ea_page_slots(c.ctx, c.shape, c.table, c.lens(some), c.lens(none), **kw)
     c.ctx.sync_status()
+
+
+def test_outputs_that_overlap_other_buffers_are_refused(ea):                                    # noqa: F811
+    c = make(ea, (8, 2, 128), 16, [1, 1], [[200, 300], [40, 50]])
+    want, want_lse = attend(ea, c, want_lse=True)
+    both = torch.zeros(4, 8, 128, dtype=torch.bfloat16, device="cuda")
+    both[:2] = c.q
+    held = [x.clone() for x in (c.k, c.v, c.table, c.free, c.n_free)]
+
+    def refused(call):
+        with pytest.raises(ea.EAError) as e:
+            call()
+        assert e.value.status == 1
+
+    c.q = both[:2]
+    refused(lambda: attend(ea, c, out=c.q))
+    refused(lambda: attend(ea, c, out=both[1:3]))
+    refused(lambda: attend(ea, c, out=c.k.view(-1)[:2048].view(2, 8, 128)))
+    refused(lambda: attend(ea, c, out=both[2:], lse=both[2:].view(-1)[:32].view(torch.float32).view(2, 8)))
+    out, lse = attend(ea, c, out=both[2:], want_lse=True)                        # side by side is no overlap
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    rows, slots = c.k.view(-1, 128), i32([1, 0])
+    fresh = torch.zeros(2, 128, dtype=torch.bfloat16, device="cuda")
+    refused(lambda: ea.ea_page_store(c.ctx, c.shape, slots, rows[:2], fresh, c.k, c.v))
+    refused(lambda: ea.ea_page_store(c.ctx, c.shape, slots, fresh, c.v.view(-1, 128)[-2:], c.k, c.v))
+    refused(lambda: ea.ea_page_store(c.ctx, c.shape, slots, fresh, fresh, c.k, c.k))
+    refused(lambda: ea.ea_page_load(c.ctx, c.shape, slots, c.k, c.v, rows[:2], fresh))
+    refused(lambda: ea.ea_page_load(c.ctx, c.shape, slots, c.k, c.v, fresh, fresh))
+    longer = c.kv_lens + 1
+    refused(lambda: ea.ea_page_plan(c.ctx, c.shape, c.kv_lens, longer, c.table, c.free, c.n_free, slots=c.free))
+    refused(lambda: ea.ea_page_plan(c.ctx, c.shape, c.kv_lens, longer, c.table, c.free, c.n_free, n_slots=8, offsets=c.table.view(-1)[:5]))
+    refused(lambda: ea.ea_page_slots(c.ctx, c.shape, c.table, c.kv_lens, longer, slots=c.table.view(-1)))
+    c.ctx.sync_status()
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(held, (c.k, c.v, c.table, c.free, c.n_free)))
+    ea.ea_page_plan(c.ctx, c.shape, c.kv_lens, c.kv_lens, c.table, c.free, c.n_free, n_slots=1)     # inputs may be the same
+    got, _ = ea.ea_page_load(c.ctx, c.shape, slots, c.k, c.k)                                       # so may pools that are read
+    assert torch.equal(got.view(torch.uint8), rows[[1, 0]].view(torch.uint8))
+    c.ctx.sync_status()
