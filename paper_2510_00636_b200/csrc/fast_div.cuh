@@ -10,7 +10,7 @@ struct FastDiv {
 };
 static inline FastDiv fast_div(int d) {
     int l = 0;
-    while ((1 << l) < d) ++l;
+    while ((1u << l) < (uint32_t)d) ++l;
     return {d == 1 ? 0u : (uint32_t)(((1ull << (31 + l)) + (uint32_t)d - 1) / (uint32_t)d), l - 1, d};
 }
 __device__ __forceinline__ int quotient(int n, const FastDiv& f) { return f.shift < 0 ? n : (int)(__umulhi((uint32_t)n, f.mul) >> f.shift); }

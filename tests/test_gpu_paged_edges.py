@@ -190,3 +190,14 @@ def test_outputs_that_overlap_other_buffers_are_refused(ea):                    
     got, _ = ea.ea_page_load(c.ctx, c.shape, slots, c.k, c.k)                                       # so may pools that are read
     assert torch.equal(got.view(torch.uint8), rows[[1, 0]].view(torch.uint8))
     c.ctx.sync_status()
+
+
+@pytest.mark.parametrize("order", [0, 1])
+def test_a_plan_of_no_sequences_with_any_head_count(ea, order):                                 # noqa: F811
+    shape = ea.make_paged_shape(0, 2 ** 30 + 1, 2 ** 30 + 1, 64, 16, 3, 4)
+    ctx = ea.Context(0, ea.ea_paged_workspace_bytes(shape))
+    none = torch.empty(0, 2 ** 30 + 1, dtype=torch.int32, device="cuda")
+    slots, offsets = ea.ea_page_plan(ctx, shape, none, none, none.view(0, 2 ** 30 + 1, 1).expand(0, 2 ** 30 + 1, 4).contiguous(), i32([0, 1, 2]),
+                                     i32([3]), n_slots=2, order=order)
+    ctx.sync_status()
+    assert slots.tolist() == [-1, -1] and offsets.tolist() == [0]

@@ -1,7 +1,10 @@
 """Refusals of the paged-cache calls at the edges of their arguments, without a GPU."""
 import ctypes
+import subprocess
 
 import pytest
+
+from paper_2510_00636_b200 import build
 
 from test_paged_host import INVALID, P, _vary, ctx, ea, shape          # noqa: F401 (fixtures)
 
@@ -17,3 +20,41 @@ def test_rows_that_overlap_what_is_written_are_refused(ea, ctx):       # noqa: F
     good = [P, 4, M, 2 * M, 4 * M, 5 * M]                              # slots, rows, k_pages, v_pages, k, v
     for change in ({4: M}, {5: 2 * M + 16368}, {4: 5 * M}, {4: 5 * M + 512}, {5: P}):
         assert L.ea_page_load(ctx, ref, *_vary(good, change), None) == INVALID, change
+
+
+def _host_program(tmp_path, source):
+    """A program that includes the library's device headers, for the CPU."""
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text(source)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    return exe
+
+
+def test_division_by_any_head_count(tmp_path):
+    """quotient(n, fast_div(d)) is n / d for every 0 <= n < 2^31 and 1 <= d < 2^31: around the multiples, and at random."""
+    exe = _host_program(tmp_path, """
+        #define __device__
+        #define __forceinline__ inline
+        #include <stdint.h>
+        static inline uint32_t __umulhi(uint32_t a, uint32_t b) { return (uint32_t)(((uint64_t)a * b) >> 32); }
+        #include "fast_div.cuh"
+        #include <stdio.h>
+        static uint64_t s = 1;
+        static uint32_t rnd() { s = s * 6364136223846793005ull + 1442695040888963407ull; return (uint32_t)(s >> 33); }
+        int main() {
+            const uint32_t top = 0x7fffffffu;
+            for (int i = 0; i < 400000; ++i) {
+                uint32_t d = i < 31 ? 1u << i : i < 62 ? (1u << (i - 31)) + 1u : i < 93 ? (2u << (i - 62)) - 1u : i < 200 ? top - (i - 93) : rnd() >> (rnd() % 31);
+                if (d < 1 || d > top) continue;
+                const FastDiv f = fast_div((int)d);
+                for (int k = 0; k < 40; ++k) {
+                    const uint64_t m = (uint64_t)(rnd() % (top / d + 1)) * d + (k % 3) - 1;
+                    const uint32_t n = k < 30 ? (uint32_t)m : k == 30 ? top : k == 31 ? 0 : rnd();
+                    if (m > top && k < 30) continue;
+                    if (quotient((int)n, f) != (int)(n / d)) { printf("%u / %u\\n", n, d); return 1; }
+                }
+            }
+            return 0;
+        }
+        """)
+    assert subprocess.run([str(exe)], timeout=60).returncode == 0
