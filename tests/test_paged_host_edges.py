@@ -1,5 +1,7 @@
 """Refusals of the paged-cache calls at the edges of their arguments, without a GPU."""
 import ctypes
+import os
+import shutil
 import subprocess
 
 import pytest
@@ -58,3 +60,21 @@ def test_division_by_any_head_count(tmp_path):
         }
         """)
     assert subprocess.run([str(exe)], timeout=60).returncode == 0
+
+
+@pytest.mark.parametrize("folder,name", [("csrc", n) for n in ("paged_attn.cuh", "fast_div.cuh", "ptx_sm100.cuh", "paged.h", "paged.cu")] +
+                         [("include", "ea.h")])
+def test_a_changed_source_makes_the_library_stale(tmp_path, monkeypatch, folder, name):
+    """Headers hold device code too: a library older than any of them is not the sources'."""
+    for d, attr in ((build.CSRC, "CSRC"), (build.INCLUDE, "INCLUDE")):
+        copy = tmp_path / os.path.basename(d)
+        shutil.copytree(d, copy)
+        monkeypatch.setattr(build, attr, str(copy))
+    library = tmp_path / "libea.so"
+    library.write_bytes(b"")
+    monkeypatch.setattr(build, "LIB_PATH", str(library))
+    now = max(p.stat().st_mtime for p in tmp_path.rglob("*") if p.is_file())
+    os.utime(library, (now + 10, now + 10))
+    assert not build._stale()
+    os.utime(tmp_path / folder / name, (now + 20, now + 20))
+    assert build._stale()
