@@ -1,11 +1,12 @@
 """Paged cache at the edges of its range: scores beyond 32 bits, and what else a call may meet."""
 import math
+import random
 
 import pytest
 import torch
 
 import paged_reference as ref
-from test_gpu_paged import Cache, attend, ea, i32, make          # noqa: F401 (a fixture)
+from test_gpu_paged import Cache, attend, check, ea, i32, make          # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -201,3 +202,165 @@ def test_a_plan_of_no_sequences_with_any_head_count(ea, order):                 
                                      i32([3]), n_slots=2, order=order)
     ctx.sync_status()
     assert slots.tolist() == [-1, -1] and offsets.tolist() == [0]
+
+
+# ---- parts of the kernels that other tests do not reach ------------------------------------------------------------
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("Hq,Hkv,m", [(9, 1, 1), (5, 1, 3), (16, 2, 2), (16, 1, 1), (1, 1, 16), (33, 3, 1), (26, 2, 1)])
+@pytest.mark.parametrize("page", [16, 128])
+def test_nine_to_sixteen_rows_of_a_list(ea, d, Hq, Hkv, m, page):                               # noqa: F811
+    """The upper half of the few-row kernel's tile: whole lists, lists shared by many CTAs, and many lists."""
+    for lens in ([[40 + 7 * g for g in range(Hkv)], [m] * Hkv, [0] * Hkv], [[60000 + g for g in range(Hkv)]],
+                 [[900 + (31 * s + 17 * g) % 300 for g in range(Hkv)] for s in range(70)]):
+        for causal in (True, False):
+            check(ea, make(ea, (Hq, Hkv, d), page, [m] * len(lens), lens), causal=causal)
+
+
+@pytest.mark.parametrize("lists,most,page", [(3000, 100, 16), (4096, 40, 16), (40, 9000, 32), (1, 30000, 16)])
+def test_plans_without_a_slot_map_over_many_processors(ea, lists, most, page):                  # noqa: F811
+    """Pools of more than 1024 pages: growing and shrinking lists mixed, pages pushed, the free count by the CTA that ends last."""
+    rng = random.Random(lists)
+    c = Cache(ea, lists, 1, 1, 64, page, lists * ref.ceil_div(most, page) + 3, ref.ceil_div(most, page))
+    old = [0] * lists
+    for _ in range(6):
+        new = [rng.choice((o, 0, most, rng.randint(0, most))) for o in old]
+        assert c.plan(old, new) is None
+        assert c.py.resize(old, new)
+        c.same()
+        old = new
+    c.ctx.sync_status()
+
+
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("seqs,each,capacity", [(3, 4000, 40001), (30, 3000, 300003)])
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_slot_maps_that_begin_at_any_word(ea, order, seqs, each, capacity, shift):              # noqa: F811
+    Hkv, page = 3, 16
+    wide = ref.ceil_div(each, page)
+    c = Cache(ea, seqs, Hkv, Hkv, 64, page, seqs * Hkv * wide, wide)
+    old, new = [0] * (seqs * Hkv), [each - 5 * (r // Hkv) for r in range(seqs * Hkv)]
+    got, again = (torch.full((capacity + 8,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    _, offsets = c.plan(old, new, slots=got[shift:shift + capacity], order=order)
+    assert c.py.resize(old, new)
+    rows, want_offsets = c.py.slots(old, new, Hkv if order else None)
+    assert offsets.tolist() == want_offsets
+    want = torch.full((capacity + 8,), 77, dtype=torch.int32)
+    want[shift:shift + capacity] = -1
+    want[shift:shift + len(rows)] = torch.tensor(rows, dtype=torch.int32)
+    assert torch.equal(got.cpu(), want)
+    ea.ea_page_slots(c.ctx, c.shape, c.table, c.lens(old), c.lens(new), slots=again[shift:shift + capacity], order=order)
+    assert torch.equal(again, got)
+    c.ctx.sync_status()
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128), (16, 8, 256)])
+@pytest.mark.parametrize("max_q", [3, 64, 300])
+def test_a_padded_batch(ea, heads, max_q):                                                      # noqa: F811
+    """A captured batch is launched for more tokens, and more sequences, than a step has."""
+    S, Hkv = 60, heads[1]
+    chunks = [0] * S
+    chunks[0], chunks[1], chunks[31], chunks[59] = 1, 3, 1, 2
+    lens = [[(700 + 13 * s + 5 * g) if s % 2 else 0 for g in range(Hkv)] for s in range(S)]
+    c = make(ea, heads, 16, chunks, lens, n_tokens=400, max_q=max_q)
+    c.ctx = ea.Context(0, ea.ea_paged_workspace_bytes(c.shape, max_q))
+    out = torch.full((400, heads[0], heads[2]), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((400, heads[0]), 7.0, device="cuda")
+    check(ea, c, out=out, lse=lse)
+    assert bool((out[7:] == 7).all()) and bool((lse[7:] == 7).all())
+
+
+# ---- as they are used ------------------------------------------------------------------------------------------------
+def test_a_cache_through_two_compressions_with_generation_in_a_graph(ea):                       # noqa: F811
+    """A prompt's cache compressed over all heads of a layer into pages, sixteen tokens generated as replays of one graph, every
+    list (they differ in length) scored and compressed again, stored back, and one more token."""
+    S, Hq, Hkv, d, n, W, n_kept, page, steps = 2, 8, 2, 128, 512, 16, 192, 16, 16
+    G = Hq // Hkv
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    rnd = lambda *shape: torch.randn(*shape, generator=gen, device="cuda").to(torch.bfloat16)      # noqa: E731
+    q_win, k, v = rnd(S, Hq, W, d), rnd(S, Hkv, n, d), rnd(S, Hkv, n, d)
+    dense = ea.make_shape(S, Hq, Hkv, d, n, W)
+    wide = ref.ceil_div(Hkv * n_kept + steps, page)
+    paged = ea.make_paged_shape(S, Hq, Hkv, d, page, S * Hkv * wide, wide)
+    longest = ea.make_shape(1, G, 1, d, wide * page, W)
+    ctx = ea.Context(0, max(ea.ea_workspace_bytes(dense), ea.ea_workspace_bytes(longest), ea.ea_paged_workspace_bytes(paged, 1)))
+    pos = torch.full((S,), n, dtype=torch.int64, device="cuda")
+    scores = ea.ea_score(ctx, dense, k, v, *ea.ea_query_stats(ctx, dense, q_win, pos, 64, 1e6), 0.02)
+    idx, head_off, k_out, v_out = ea.ea_select_compact_adaptive(ctx, dense, scores, n_kept, ea.ea_n_floor(n_kept, 0.2), k, v)
+    lens = (head_off[:, 1:] - head_off[:, :-1]).to(torch.int32).contiguous()
+    table = torch.full((S, Hkv, wide), -1, dtype=torch.int32, device="cuda")
+    free, n_free = torch.arange(S * Hkv * wide, dtype=torch.int32, device="cuda"), i32([S * Hkv * wide])
+    kp, vp = (torch.full((S * Hkv * wide, page, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    zero = torch.zeros_like(lens)
+    slots, _ = ea.ea_page_plan(ctx, paged, zero, lens, table, free, n_free, n_slots=S * Hkv * n_kept)
+    ea.ea_page_store(ctx, paged, slots, k_out.view(-1, d), v_out.view(-1, d), kp, vp)
+    rows = {(s, g): [x[s, int(head_off[s, g]):int(head_off[s, g + 1])] for x in (k_out, v_out)] for s in range(S) for g in range(Hkv)}
+
+    q, kn, vn = (torch.zeros(S, h, d, dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv))
+    longer, out = torch.empty_like(lens), torch.empty_like(q)
+    one, off = torch.empty(S * Hkv, dtype=torch.int32, device="cuda"), torch.empty(S + 1, dtype=torch.int32, device="cuda")
+
+    def step():
+        torch.add(lens, 1, out=longer)
+        ea.ea_page_plan(ctx, paged, lens, longer, table, free, n_free, order=ea.SLOTS_BY_TOKEN, slots=one, offsets=off)
+        ea.ea_page_store(ctx, paged, one, kn, vn, kp, vp)
+        ea.ea_paged_attention(ctx, paged, q, off, 1, longer, table, kp, vp, out=out)
+        lens.copy_(longer)
+
+    def attended():
+        ctx.sync_status()
+        exact = ref.attention(q, off, lens, lambda s, g: rows[s, g], d ** -0.5, True)
+        assert bool(((out.double() - exact[0]).abs() <= ref.attention_tolerance(*exact, int(lens.max()))[0]).all())
+
+    kept = [x.clone() for x in (lens, table, free, n_free, kp, vp)]
+    step()
+    for x, y in zip((lens, table, free, n_free, kp, vp), kept):
+        x.copy_(y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for x, y in zip((lens, table, free, n_free, kp, vp), kept):
+        x.copy_(y)
+    window = []
+    for _ in range(steps):
+        for x in (q, kn, vn):
+            x.copy_(rnd(*x.shape))
+        window.append(q.clone())
+        graph.replay()
+        for (s, g), pair in rows.items():
+            pair[:] = [torch.cat([pair[0], kn[s, g][None]]), torch.cat([pair[1], vn[s, g][None]])]
+        attended()
+    # the next compression: half of every list, scored with the window of the queries since
+    q_win = torch.stack(window, 2)                                                              # [S, Hq, W, d]
+    slots, offsets = ea.ea_page_slots(ctx, paged, table, zero, lens, n_slots=int(lens.sum()))
+    kd, vd = ea.ea_page_load(ctx, paged, slots, kp, vp)
+    ends, half, new = offsets.tolist(), [], {}
+    for i, (s, g) in enumerate(sorted(rows)):
+        a, b = ends[i], ends[i + 1]
+        assert torch.equal(kd[a:b], rows[s, g][0]) and torch.equal(vd[a:b], rows[s, g][1])
+        m = b - a
+        one_list = ea.make_shape(1, G, 1, d, m, W)
+        kr, vr = kd[a:b].view(1, 1, m, d), vd[a:b].view(1, 1, m, d)
+        stats = ea.ea_query_stats(ctx, one_list, q_win[s:s + 1, g * G:(g + 1) * G].contiguous(), pos[:1] + steps, 64, 1e6)
+        scores = ea.ea_score(ctx, one_list, kr, vr, *stats, 0.02)
+        idx, ko, vo = ea.ea_select_compact(ctx, one_list, scores, m // 2, kr, vr)
+        top = scores.view(-1).sort(descending=True, stable=True).indices[:m // 2].sort().values
+        assert torch.equal(idx.view(-1).long(), top)
+        half.append(m // 2)
+        new[s, g] = [ko.view(-1, d), vo.view(-1, d)]
+        assert torch.equal(new[s, g][0], rows[s, g][0][top]) and torch.equal(new[s, g][1], rows[s, g][1][top])
+    rows = new
+    fewer = i32(half, S, Hkv)
+    before = n_free.item()
+    ea.ea_page_plan(ctx, paged, lens, fewer, table, free, n_free)
+    slots, _ = ea.ea_page_slots(ctx, paged, table, zero, fewer, n_slots=sum(half))
+    ea.ea_page_store(ctx, paged, slots, torch.cat([rows[x][0] for x in sorted(rows)]), torch.cat([rows[x][1] for x in sorted(rows)]), kp, vp)
+    assert n_free.item() - before == int(((lens + page - 1) // page - (fewer + page - 1) // page).sum())
+    lens.copy_(fewer)
+    for x in (q, kn, vn):
+        x.copy_(rnd(*x.shape))
+    graph.replay()                                          # the same graph over the compressed lists
+    for (s, g), pair in rows.items():
+        pair[:] = [torch.cat([pair[0], kn[s, g][None]]), torch.cat([pair[1], vn[s, g][None]])]
+    attended()
+    held = table[table >= 0].tolist()
+    assert len(set(held)) == len(held) and not set(held) & set(free[:n_free.item()].tolist())
