@@ -33,13 +33,13 @@ import torch  # noqa: E402
 from paper_2510_00636_b200 import inputs  # noqa: E402
 
 # dram__bytes_read.sum + dram__bytes_write.sum of one launch of the log-score kernel divided by the
-# key-slots of that launch (one ncu --set full capture per shape on a few layers, clocks not locked),
+# key-slots of that launch (one ncu capture per shape on a few layers, clocks not locked),
 # keyed by (head_dim, query heads per KV head, cache format): the log-score write, the sharing of key
 # tiles and the bytes of a key depend on them.  NCU_CAPTURE_SOURCE is the fingerprint of the kernel
 # source that was captured.
-NCU_DRAM_BYTES_PER_KEY_SLOT = {(256, 2, "bf16"): 1.101994e9 / 2097152, (128, 4, "bf16"): 293.660e6 / 1048576,
-                               (256, 2, "fp8"): 563.424e6 / 2097152}
-NCU_CAPTURE_SOURCE = "e185e5558dd2cd61"
+NCU_DRAM_BYTES_PER_KEY_SLOT = {(256, 2, "bf16"): 1.101786e9 / 2097152, (128, 4, "bf16"): 293.563e6 / 1048576,
+                               (256, 2, "fp8"): 563.328e6 / 2097152}
+NCU_CAPTURE_SOURCE = "050b831ba3d49285"
 # nominal figures of the part, reported beside the measured denominators
 NOMINAL_HBM_GBS, NOMINAL_TFLOPS = 8000.0, 2250.0
 
