@@ -269,6 +269,25 @@ def test_a_padded_batch(ea, heads, max_q):                                      
     assert bool((out[7:] == 7).all()) and bool((lse[7:] == 7).all())
 
 
+@pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128), (16, 8, 256)])
+def test_one_step_as_a_call_for_each_run_of_sequences(ea, heads):                               # noqa: F811
+    """Single tokens in a call of their own beside a prompt's chunk: the same tokens, offsets and outputs, by runs."""
+    Hkv = heads[1]
+    chunks = [1] * 6 + [130] + [1, 0, 1]
+    lens = [[max(m, 1) + (s * 53 + g * 97) % 400 for g in range(Hkv)] for s, m in enumerate(chunks)]
+    c = make(ea, heads, 16, chunks, lens, n_tokens=sum(chunks) + 3)
+    out, lse = torch.full_like(c.q, 7.0), torch.full(c.q.shape[:2], 7.0, device="cuda")
+    for a, b, max_q in ((0, 6, 1), (6, 7, 130), (7, 10, 1)):
+        run = ea.make_paged_shape(b - a, *heads, 16, c.k.shape[0], c.table.shape[2])
+        ea.ea_paged_attention(c.ctx, run, c.q, c.q_offsets[a:b + 1], max_q, c.kv_lens[a:b], c.table[a:b], c.k, c.v, out=out, lse=lse)
+    c.ctx.sync_status()
+    n = sum(chunks)
+    exact = ref.attention(c.q, c.q_offsets, c.kv_lens, c.rows_of, c.d ** -0.5, True)
+    tol_o, tol_l = ref.attention_tolerance(*exact, int(c.kv_lens.max()))
+    assert bool(((out.double() - exact[0]).abs() <= tol_o)[:n].all()) and bool(((lse.double() - exact[1]).abs() <= tol_l)[:n].all())
+    assert bool((out[n:] == 7).all()) and bool((lse[n:] == 7).all())
+
+
 # ---- as they are used ------------------------------------------------------------------------------------------------
 def test_a_cache_through_two_compressions_with_generation_in_a_graph(ea):                       # noqa: F811
     """A prompt's cache compressed over all heads of a layer into pages, sixteen tokens generated as replays of one graph, every
