@@ -530,6 +530,10 @@ int64_t ea_n_floor(int64_t n_kept, double safeguard);
  * some that do not fit records EA_ERR_PAGES, which ea_sync_status reports, and
  * touches no memory outside the buffers described here.
  *
+ * The scoring and compaction calls take one length per call: lists of different lengths
+ * are read back with ea_page_load and compressed again one at a time, their lengths
+ * known to the host.
+ *
  * Limits (EA_ERR_UNSUPPORTED beyond): page_rows 16, 32, 64 or 128; head_dim 64,
  * 128 or 256; n_seqs * n_kv_heads <= 65535; n_pages * page_rows < 2^31;
  * max_pages * page_rows <= 2^30; n_tokens * n_q_heads < 2^31.  The calls that use
@@ -633,6 +637,10 @@ ea_status ea_page_load(ea_ctx* ctx, const ea_paged_shape* shape, const int32_t* 
  * ones of a sequence sees, with causal != 0, the rows p <= n - m + i of a list of n
  * rows (evicted rows left no gap: order is all that counts), with causal = 0 all n.
  * A token that sees no row gets zeros and lse = -infinity.
+ * The kernel is chosen by max_q * G for the whole call: up to 16 rows per list it reads K and V
+ * at memory bandwidth, beyond, every sequence takes part in tiles of 128 or 256 rows.  A step
+ * that holds a prompt's chunk and many single tokens is faster as two calls, each for
+ * a run of sequences (its own shape, with lengths, table and offsets that begin there).
  *
  * q          bf16 [n_tokens, Hq, d], POST-RoPE, 16-byte aligned; q_stride: elements between
  *            tokens (0 = dense), a multiple of 8 of at least Hq * d

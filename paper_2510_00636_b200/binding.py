@@ -701,8 +701,8 @@ def _slot_map(shape, order, n_slots, slots, offsets, device, like):
 def ea_page_plan(ctx: Context, shape: PagedShape, old_lens, new_lens, block_table, free_pages, n_free, n_slots=None,
                  order: int = SLOTS_BY_LIST, slots=None, offsets=None):
     """Takes and gives back pages as the lists' lengths (int32 [S,Hkv]) change; ``block_table`` int32 [S,Hkv,max_pages],
-    ``free_pages`` int32 [n_pages] and ``n_free`` int32 [1] are updated.  With ``n_slots`` (capacity of the slot map) or
-    ``slots`` returns (slots, offsets) of the new rows, else None."""
+    ``free_pages`` int32 [n_pages] and ``n_free`` int32 [1] are updated.  With ``n_slots`` (capacity of the slot map; 0: no list
+    may grow) or ``slots`` returns (slots, offsets) of the new rows, else None."""
     S, Hkv, dev, i32 = shape.n_seqs, shape.n_kv_heads, ctx.device_index, torch.int32
     a_old = _address(old_lens, i32, (S, Hkv), dev, "old_lens")
     a_new = _address(new_lens, i32, (S, Hkv), dev, "new_lens")
@@ -794,7 +794,8 @@ def ea_paged_attention(ctx: Context, shape: PagedShape, q, q_offsets, max_q: int
                        scale: float | None = None, causal: bool = True, out=None, lse=None, want_lse: bool = False):
     """Attention of new tokens ``q`` bf16 [T,Hq,d] (tokens any distance apart; sequence s owns ``q_offsets[s] ..
     q_offsets[s+1]``, int32 [S+1], at most ``max_q`` tokens each) over the lists of ``kv_lens`` int32 [S,Hkv] rows ->
-    out bf16 [T,Hq,d] (and lse fp32 [T,Hq] if asked).  The new tokens' own pairs are the last rows of the lists."""
+    out bf16 [T,Hq,d] (and lse fp32 [T,Hq] if asked).  The new tokens' own pairs are the last rows of the lists.  A token whose
+    largest score is 7e8 or more in magnitude gets NaN; ``out`` and ``lse`` may overlap nothing that the call reads."""
     S, Hq, Hkv, d, dev, i32 = shape.n_seqs, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, ctx.device_index, torch.int32
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError(f"q: expected [tokens, {Hq}, {d}]")

@@ -23,9 +23,10 @@ namespace {
 // the product with its 16 value rows.  At head_dim <= 128 a second group of four warps takes every other block: a block is a
 // chain of some 1300 cycles for a warp, about as long as its bytes take to arrive.  No barrier among the warps until the
 // list ends, where they are merged in a fixed order.  At most 16 of the 128 rows of a tcgen05 tile would be in use here,
-// and the limit is memory: 32 sequences of up to 16 384 tokens, 28 heads on 4 lists of head_dim 128, 676 MB: 107 to 112 us
-// = 6.0 to 6.3 TB/s (0.94 to 0.98 of the measured copy rate); one sequence of 4096 tokens on 8 lists, 16.8 MB: 13 us, most of it
-// the latencies of the share's start, of four blocks per CTA and of the join.
+// and the limit is memory: 32 sequences of up to 16 384 tokens, 28 heads on 4 lists of head_dim 128, 676 MB: 113 us called one
+// after the other, 106 in a graph = 6.0 and 6.4 TB/s (0.92 and 0.98 of the measured copy rate); one sequence of 4096 tokens on
+// 8 lists, 16.8 MB: 15 and 13 us, most of it the latencies of the share's start, of four blocks per CTA and of the join.
+// At head_dim 64 a block takes as long for half the bytes, and the same 676 MB take 140 us = 4.8 TB/s (0.75 of the copy rate).
 template <int D> struct Few {
     static constexpr int GROUPS = D == 256 ? 1 : 2;
     static constexpr int NW = 4 * GROUPS;

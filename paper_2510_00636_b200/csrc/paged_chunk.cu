@@ -7,8 +7,9 @@
 // head_dim <= 128: two row tiles against blocks of 64 keys (S, P and O of both fill the 512 columns of tensor memory).
 // head_dim 256: O of one tile takes half of them, so there is one tile, against blocks of 128 keys, and two CTAs of a
 // cluster work as one (cta_group::2): 256 rows, each CTA with its 128, half of a block's keys of K and half of V's
-// channels.  What an SM can draw from L2 (26 to 29 bytes per cycle) is the limit there: a CTA alone fetches 64 KiB of K and
-// V for 128 rows and 64 keys, a CTA of the pair half of that (512 tokens over 16 384 keys, 8 lists: 206 -> 122 us).
+// channels.  What an SM can draw from L2 (26 to 29 bytes per cycle) was the limit of a CTA alone, which fetches 64 KiB of K and
+// V for 128 rows and 64 keys; a CTA of the pair fetches half of that (512 tokens over 16 384 keys, 8 lists: 206 -> 122 us, the
+// tensor pipe 67 % busy).  The last row tile of a list costs as much as a full one: 517 tokens take 148 us where 512 take 125.
 //
 // Two warps keep K and V flowing through a ring of slots each (TMA boxes of a page), one warp per row tile issues its MMAs
 // (the waits of one are hidden by the other's; in a pair one warp of the first CTA issues for both), eight warps do the
@@ -26,7 +27,8 @@
 // query rows from shared memory for only 64 columns: 48 cycles an instruction where the arithmetic takes 32), the
 // exponentials 1024 of the special function units; the two tiles alternate on both and about 1600 pass.  2048 tokens
 // over 32 768 keys, 32 heads on 8 lists: 880 us = 1.21 PFLOP/s (0.72 of the measured cuBLAS rate); back to back, at the
-// clock that the power limit leaves, 1040 to 1070 us (0.71 to 0.74 of the rate measured there).
+// clock that the power limit leaves, 1040 to 1080 us (0.70 to 0.73 of the rate measured there).  At head_dim 64 the exponentials
+// are the larger part: 1024 tokens over 16 384 keys take 194 us, the special function units 68 % busy, the tensor pipe 34 %.
 #include <type_traits>
 
 #include "paged.h"

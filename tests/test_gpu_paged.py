@@ -52,7 +52,7 @@ class Cache:
 
 
 # ---- plans and slots -------------------------------------------------------------------------------------------------
-# one CTA; a cluster; three launches (many slots); more lists than a CTA scans itself
+# a cluster; three launches (many slots); more lists than a CTA scans itself
 @pytest.mark.parametrize("seqs,Hkv,page,most,rounds,capacity", [
     (1, 1, 16, 40, 12, 64), (5, 3, 16, 100, 10, 1600), (7, 8, 32, 300, 6, 20000), (3, 4, 128, 9000, 4, 120000),
     (600, 7, 64, 70, 3, 300000), (16383, 4, 16, 20, 2, 1 << 21)])
